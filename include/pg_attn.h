@@ -244,6 +244,122 @@ int pg_grouped_positions(int n_groups, int n_suffixes, int total_prefix, int tot
                          void* stream);
 
 /*
+ * Linear attention with a decay for each key/value head, over the same shared prefixes: layers of hybrid models
+ * that keep a state instead of a key/value cache. With l = exp(log_decay[kv head]), c = scale and the keys a row
+ * sees as in pg_attn_fwd (prefix row t: prefix keys 0..t; response row j: the whole prefix, then its own 0..j),
+ *   o_t = c sum_s l^(t - s) (q_t . k_s) v_s,    t - s: the distance of their positions,
+ * which is the recurrence S_t = l S_{t-1} + k_t v_t^T, o_t = c S_t^T q_t. The prefix is walked once; every member
+ * starts from the state it ends with. Tensors, grouping arrays, types, head geometry, ownership, determinism and
+ * errors are those of pg_attn_fwd; all tensor pointers and the workspace are 16-byte aligned.
+ *
+ * log_decay: float [h_kv] (device), natural logarithms, <= 0; 0 keeps everything, -inf keeps only the row itself
+ * (values above 0 or NaN are not checked; results are then unspecified). It is a constant of the layer: no gradient.
+ * A state is float [head_dim of k, head_dim of v]; sums are held in fp32. A non-finite value of a row reaches, beside
+ * the rows that see it, the other rows of its 64-row piece of the segment.
+ *
+ * Forward: writes o_pre, o_suf. state_in [n_groups, h_kv, head_dim, head_dim] (or NULL for zeros) is the state before
+ * each group's prefix: a prompt can be read in pieces. state_pre [n_groups, ...] and state_suf [n_suffixes, ...]
+ * (both or neither may be NULL) receive the states after each prefix and after each response (an empty response: its
+ * prefix's), from which pg_linear_step goes on. They must not overlap state_in.
+ */
+size_t pg_linear_fwd_workspace_size(int n_groups, int n_suffixes, int total_prefix, int total_suffix, int h_q,
+                                    int h_kv, int head_dim);
+
+int pg_linear_fwd(int dtype, int n_groups, int n_suffixes, int total_prefix, int total_suffix,
+                  const int32_t* cu_prefix_lens, const int32_t* cu_suffix_lens, const int32_t* group_sizes,
+                  int h_q, int h_kv, int head_dim, float scale, const float* log_decay,
+                  const void* q_pre, const void* k_pre, const void* v_pre,
+                  const void* q_suf, const void* k_suf, const void* v_suf, const float* state_in,
+                  void* o_pre, void* o_suf, float* state_pre, float* state_suf,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Backward: the vector-Jacobian product of the forward without state_in (nothing of the forward is needed but its
+ * inputs). dk_pre and dv_pre are summed over the members and over the query heads that share a kv head, in a fixed
+ * order.
+ */
+size_t pg_linear_bwd_workspace_size(int n_groups, int n_suffixes, int total_prefix, int total_suffix, int h_q,
+                                    int h_kv, int head_dim);
+
+int pg_linear_bwd(int dtype, int n_groups, int n_suffixes, int total_prefix, int total_suffix,
+                  const int32_t* cu_prefix_lens, const int32_t* cu_suffix_lens, const int32_t* group_sizes,
+                  int h_q, int h_kv, int head_dim, float scale, const float* log_decay,
+                  const void* q_pre, const void* k_pre, const void* v_pre,
+                  const void* q_suf, const void* k_suf, const void* v_suf,
+                  const void* do_pre, const void* do_suf,
+                  void* dq_pre, void* dk_pre, void* dv_pre, void* dq_suf, void* dk_suf, void* dv_suf,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * One token for each of n sequences: state_out = l state + k v^T, o = c state_out^T q. q, o [n, h_q, head_dim],
+ * k, v [n, h_kv, head_dim], state, state_out float [n, h_kv, head_dim, head_dim]; state_out may be state itself (in
+ * place), no other overlap. No workspace.
+ */
+int pg_linear_step(int dtype, int n, int h_q, int h_kv, int head_dim, float scale, const float* log_decay,
+                   const void* q, const void* k, const void* v, const float* state, void* o, float* state_out,
+                   void* stream);
+
+/*
+ * Log-probabilities of the responses' tokens from the logits. Response row j of a member predicts its token j + 1;
+ * the first token of every member is predicted by the last prefix row of its group, so that row's softmax serves all
+ * members, and its gradient is the sum over them. A member's last row predicts nothing.
+ *
+ * logits_last: [n_groups, vocab], the logits of each group's last prefix row; logits_suf: [total_suffix, vocab]; dtype
+ * PG_BF16 or PG_FP32, any element alignment, stride_* >= vocab elements between rows. tokens: [total_suffix] of
+ * token_bytes 4 (int32) or 8 (int64). With x = logits / temperature of the row that predicts token r:
+ *   logp[r] = x[token] - lse[r],  lse[r] = ln sum exp x,  entropy[r] = -sum p ln p   (float [total_suffix]).
+ * entropy may be NULL (it is for monitoring and has no gradient). A token outside [0, vocab) (padding) gets logp 0
+ * and no gradient. Logits of -inf are legal; a row of nothing else gives logp = lse = -inf, entropy 0 and a zero
+ * gradient. Where a prefix is empty nothing predicts its members' first tokens: logp 0, lse -inf, entropy 0, and that
+ * row of logits_last is not read.
+ *
+ * The gradient: dlogits = (1 / temperature) sum over the row's targets of dlogp (onehot - softmax), with lse as the
+ * forward wrote it. Every row of dlogits_last and dlogits_suf is written (zeros where nothing is predicted, or where
+ * the row's targets all have dlogp 0: such a row is not read), [0, vocab) of it only. dlogits_* may be logits_*
+ * themselves with the same stride (in place), no other overlap.
+ */
+size_t pg_token_logprobs_workspace_size(int n_groups, int n_suffixes, int total_suffix, int vocab);
+
+int pg_token_logprobs(int dtype, int token_bytes, int n_groups, int n_suffixes, int total_prefix, int total_suffix,
+                      const int32_t* cu_prefix_lens, const int32_t* cu_suffix_lens, const int32_t* group_sizes,
+                      int vocab, float temperature, const void* logits_last, int64_t stride_last,
+                      const void* logits_suf, int64_t stride_suf, const void* tokens,
+                      float* logp, float* lse, float* entropy, void* workspace, size_t workspace_bytes, void* stream);
+
+int pg_token_logprobs_bwd(int dtype, int token_bytes, int n_groups, int n_suffixes, int total_prefix,
+                          int total_suffix, const int32_t* cu_prefix_lens, const int32_t* cu_suffix_lens,
+                          const int32_t* group_sizes, int vocab, float temperature,
+                          const void* logits_last, int64_t stride_last, const void* logits_suf, int64_t stride_suf,
+                          const void* tokens, const float* lse, const float* dlogp,
+                          void* dlogits_last, int64_t dstride_last, void* dlogits_suf, int64_t dstride_suf,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The clipped policy loss with a KL term over the responses' tokens, and its gradient, in one call. With A the
+ * advantage of the token's member, r = exp(logp - logp_old), x = logp_ref - logp:
+ *   L = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + beta (exp(x) - x - 1),   loss = sum w L.
+ * PG_AVERAGE_GROUP: the mean over a member's kept tokens, then over its group's members (one without kept tokens
+ * counts, with 0), then over the groups that have members. PG_AVERAGE_TOKEN: the mean over all kept tokens.
+ *
+ * logp, logp_old, logp_ref: float [total_suffix]; logp_old may be NULL (the policy that sampled is this one: r = 1,
+ * with its gradient), logp_ref may be NULL when beta is 0 (given all the same, its term is reported).
+ * advantages: float [n_suffixes]. mask: uint8 [total_suffix], 0 drops a token (its values are not used, whatever they
+ * are), or NULL. An advantage of 0 gives a policy term of 0 whatever the ratio.
+ * stats: float [4] = loss, its policy term, the KL term (without beta), the share of clipped tokens, each weighted
+ * by w. dlogp: float [total_suffix] = grad_scale * dloss / dlogp (0 at dropped tokens), or NULL for the loss alone.
+ * clip_low in [0, 1], clip_high >= 0. The arithmetic and the sums are in fp64, in a fixed order.
+ */
+typedef enum { PG_AVERAGE_GROUP = 0, PG_AVERAGE_TOKEN = 1 } pg_average;
+
+size_t pg_policy_loss_workspace_size(int n_groups, int n_suffixes, int total_suffix);
+
+int pg_policy_loss(int average, int n_groups, int n_suffixes, int total_suffix, const int32_t* cu_suffix_lens,
+                   const int32_t* group_sizes, double clip_low, double clip_high, double beta, double grad_scale,
+                   const float* logp, const float* logp_old, const float* logp_ref, const float* advantages,
+                   const uint8_t* mask, float* stats, float* dlogp,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Kernel timing for benchmarks. Between pg_timing_start() and pg_timing_stop()
  * every call brackets each of its kernel launches with a pair of HIP events
  * recorded on the call's stream (at most 16384 launches are recorded per start;
@@ -260,7 +376,13 @@ typedef enum {
   PG_K_DQ = 4,       /* backward: dQ and rowsum(dO * O) (query-stationary)    */
   PG_K_ROPE = 5,     /* rotary embedding kernel of pg_rope                    */
   PG_K_LAST = 6,     /* pg_attn_fwd_last: chunk kernel and merge, one interval */
-  PG_K_KV_REDUCE = 7 /* backward: fixed-order sum of the prefix dK/dV partials  */
+  PG_K_KV_REDUCE = 7, /* backward: fixed-order sum of the prefix dK/dV partials */
+  PG_K_LINEAR_STATE = 8, /* linear attention: item plan, states and scans of one walk, one interval */
+  PG_K_LINEAR_OUT = 9,   /* linear attention: outputs, or dq                   */
+  PG_K_LINEAR_GRAD = 10, /* linear attention: dk, dv                           */
+  PG_K_LINEAR_STEP = 11, /* linear attention: single tokens                    */
+  PG_K_LOGPROBS = 12,    /* token log-probabilities, or their gradient         */
+  PG_K_POLICY = 13       /* policy loss: counts, terms and sums, one interval  */
 } pg_kernel;
 
 int pg_timing_start(void);
@@ -270,7 +392,8 @@ int pg_timing_get(int kernel, int* launches, double* total_ms);
 /*
  * Verdict of the device-side check of the grouping arrays in the last call
  * that used this workspace (pg_attn_fwd, pg_attn_bwd, their _xours forms,
- * pg_attn_fwd_last, pg_rope, pg_grouped_positions), or with workspace == NULL
+ * pg_attn_fwd_last, pg_rope, pg_grouped_positions, pg_linear_fwd, pg_linear_bwd,
+ * pg_token_logprobs, its _bwd form, pg_policy_loss), or with workspace == NULL
  * the last pg_attn_fwd_noalloc on the current device: PG_OK when they were
  * consistent, PG_EINVAL when they were not (that call did no work). It waits
  * for the stream (the one that call used) to finish. PG_EWORKSPACE when the

@@ -14,6 +14,9 @@ computation is the reference the grouped kernels are checked against.
 ``rope`` is the step before the attention (Algorithm 1 takes rotary-encoded q
 and k): the rotary embedding with the repeated-layout position ids that the
 grouped layout keeps.
+
+``linear`` is linear attention with a decay over the same layout, ``policy`` the responses' log-probabilities and
+the clipped policy loss.
 """
 from .attention import (  # noqa: F401
     causal_attention,
@@ -22,3 +25,5 @@ from .attention import (  # noqa: F401
     query_rows,
 )
 from .rope import grouped_positions, inv_freq, pair_index, rope  # noqa: F401,E402
+from .linear import linear_oracle, linear_steps  # noqa: F401,E402
+from .policy import policy_loss_oracle, token_logprobs_oracle  # noqa: F401,E402

@@ -21,6 +21,7 @@ _lib = None
 
 # names and argument types of every function include/pg_attn.h declares
 _I, _Z, _F, _P = ctypes.c_int, ctypes.c_size_t, ctypes.c_float, ctypes.c_void_p
+_L, _D = ctypes.c_int64, ctypes.c_double
 SIGNATURES = {
     "pg_attn_fwd_workspace_size": (_Z, [_I, _I, _I, _I, _I, _I, _I]),
     "pg_attn_bwd_workspace_size": (_Z, [_I, _I, _I, _I, _I, _I, _I]),
@@ -34,6 +35,17 @@ SIGNATURES = {
     "pg_rope_workspace_size": (_Z, [_I]),
     "pg_rope": (_I, [_I, _I, _I, _I, _I, _P, _P, _P, _I, _I, _I, _I, ctypes.c_double, _I] + [_P] * 8 + [_P, _Z, _P]),
     "pg_grouped_positions": (_I, [_I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "pg_linear_fwd_workspace_size": (_Z, [_I, _I, _I, _I, _I, _I, _I]),
+    "pg_linear_bwd_workspace_size": (_Z, [_I, _I, _I, _I, _I, _I, _I]),
+    "pg_linear_fwd": (_I, [_I, _I, _I, _I, _I, _P, _P, _P, _I, _I, _I, _F] + [_P] * 12 + [_P, _Z, _P]),
+    "pg_linear_bwd": (_I, [_I, _I, _I, _I, _I, _P, _P, _P, _I, _I, _I, _F] + [_P] * 15 + [_P, _Z, _P]),
+    "pg_linear_step": (_I, [_I, _I, _I, _I, _I, _F] + [_P] * 8),
+    "pg_token_logprobs_workspace_size": (_Z, [_I, _I, _I, _I]),
+    "pg_token_logprobs": (_I, [_I, _I, _I, _I, _I, _I, _P, _P, _P, _I, _F, _P, _L, _P, _L, _P, _P, _P, _P, _P, _Z, _P]),
+    "pg_token_logprobs_bwd": (_I, [_I, _I, _I, _I, _I, _I, _P, _P, _P, _I, _F, _P, _L, _P, _L, _P, _P, _P, _P, _L, _P,
+                                   _L, _P, _Z, _P]),
+    "pg_policy_loss_workspace_size": (_Z, [_I, _I, _I]),
+    "pg_policy_loss": (_I, [_I, _I, _I, _I, _P, _P, _D, _D, _D, _D] + [_P] * 7 + [_P, _Z, _P]),
     "pg_timing_start": (_I, []),
     "pg_timing_stop": (_I, []),
     "pg_timing_get": (_I, [_I, ctypes.POINTER(ctypes.c_int), ctypes.POINTER(ctypes.c_double)]),
@@ -64,7 +76,8 @@ def lib():
     return _lib
 
 
-KERNELS = {"plan": 0, "fwd": 1, "dkdv": 3, "dq": 4, "rope": 5, "last": 6, "kv_reduce": 7}
+KERNELS = {"plan": 0, "fwd": 1, "dkdv": 3, "dq": 4, "rope": 5, "last": 6, "kv_reduce": 7, "linear_state": 8,
+           "linear_out": 9, "linear_grad": 10, "linear_step": 11, "logprobs": 12, "policy": 13}
 ROPE_INVERSE, ROPE_INTERLEAVED = 1, 2
 
 
@@ -363,6 +376,226 @@ def grouped_positions(total_prefix, total_suffix, cu_prefix, cu_suffix, group_si
                                     workspace.numel(), _stream(torch, dev))
     _check(st)
     return pos_pre, pos_suf
+
+
+def linear_workspace_bytes(kind: str, n_groups, n_suffixes, total_prefix, total_suffix, h_q, h_kv, head_dim) -> int:
+    fn = lib().pg_linear_fwd_workspace_size if kind == "fwd" else lib().pg_linear_bwd_workspace_size
+    return int(fn(n_groups, n_suffixes, total_prefix, total_suffix, h_q, h_kv, head_dim))
+
+
+def _grouping(device, **arrays):
+    """Grouping arrays: contiguous int32 tensors on the tensors' device, cu_* one longer than what they delimit."""
+    import torch
+    for name, (n, t) in arrays.items():
+        if t.dtype != torch.int32 or not t.is_contiguous() or t.device != device:
+            raise TypeError(f"{name} must be a contiguous int32 tensor on {device}")
+        if t.numel() != n:
+            raise ValueError(f"{name} has {t.numel()} entries, expected {n}")
+
+
+def linear_fwd(q_pre, k_pre, v_pre, q_suf, k_suf, v_suf, log_decay, cu_prefix, cu_suffix, group_sizes, scale,
+               state_in=None, states=False, out=None, workspace=None):
+    """Linear attention with a decay for each kv head over shared prefixes (pg_linear_fwd). ``log_decay`` [h_kv]
+    float32; ``state_in`` [n_groups, h_kv, d, d] float32: the states before the prefixes (None: zeros). Returns
+    (o_pre, o_suf), with ``states`` also the states after each prefix and each response."""
+    import torch
+    ng, ns, tp, ts, hq, hkv, d = _shapes(q_pre, k_pre, q_suf, cu_prefix, cu_suffix, group_sizes)
+    dev, dt = q_pre.device, q_pre.dtype
+    if out is None:
+        out = (torch.empty_like(q_pre), torch.empty_like(q_suf))
+        if states:
+            out += (torch.empty((ng, hkv, d, d), device=dev), torch.empty((ns, hkv, d, d), device=dev))
+    if workspace is None:
+        workspace = torch.empty(linear_workspace_bytes("fwd", ng, ns, tp, ts, hq, hkv, d), device=dev, dtype=torch.uint8)
+    pre, suf = (tp, hq, d), (ts, hq, d)
+    _expect(dev, dt, q_pre=(pre, q_pre), k_pre=((tp, hkv, d), k_pre), v_pre=((tp, hkv, d), v_pre), q_suf=(suf, q_suf),
+            k_suf=((ts, hkv, d), k_suf), v_suf=((ts, hkv, d), v_suf), o_pre=(pre, out[0]), o_suf=(suf, out[1]))
+    f32 = {"log_decay": ((hkv,), log_decay)}
+    if states:
+        f32.update(state_pre=((ng, hkv, d, d), out[2]), state_suf=((ns, hkv, d, d), out[3]))
+    if state_in is not None:
+        f32["state_in"] = ((ng, hkv, d, d), state_in)
+    _expect(dev, None, **f32)
+    _grouping(dev, cu_prefix=(ng + 1, cu_prefix), cu_suffix=(ns + 1, cu_suffix), group_sizes=(ng, group_sizes))
+    _workspace(workspace, dev)
+    with torch.cuda.device(dev):
+        st = lib().pg_linear_fwd(
+            _dtype_code(torch, dt), ng, ns, tp, ts, _ptr(cu_prefix), _ptr(cu_suffix), _ptr(group_sizes), hq, hkv, d,
+            float(scale), _ptr(log_decay), _ptr(q_pre), _ptr(k_pre), _ptr(v_pre), _ptr(q_suf), _ptr(k_suf), _ptr(v_suf),
+            _ptr(state_in), _ptr(out[0]), _ptr(out[1]), _ptr(out[2]) if states else None,
+            _ptr(out[3]) if states else None, _ptr(workspace), workspace.numel(), _stream(torch, dev))
+    _check(st)
+    return tuple(out[:4] if states else out[:2])
+
+
+def linear_bwd(q_pre, k_pre, v_pre, q_suf, k_suf, v_suf, do_pre, do_suf, log_decay, cu_prefix, cu_suffix, group_sizes,
+               scale, out=None, workspace=None):
+    """Backward of linear_fwd without state_in (pg_linear_bwd): (dq_pre, dk_pre, dv_pre, dq_suf, dk_suf, dv_suf)."""
+    import torch
+    ng, ns, tp, ts, hq, hkv, d = _shapes(q_pre, k_pre, q_suf, cu_prefix, cu_suffix, group_sizes)
+    dev, dt = q_pre.device, q_pre.dtype
+    if out is None:
+        out = tuple(torch.empty_like(t) for t in (q_pre, k_pre, v_pre, q_suf, k_suf, v_suf))
+    if workspace is None:
+        workspace = torch.empty(linear_workspace_bytes("bwd", ng, ns, tp, ts, hq, hkv, d), device=dev, dtype=torch.uint8)
+    pre_q, pre_kv, suf_q, suf_kv = (tp, hq, d), (tp, hkv, d), (ts, hq, d), (ts, hkv, d)
+    _expect(dev, dt, q_pre=(pre_q, q_pre), k_pre=(pre_kv, k_pre), v_pre=(pre_kv, v_pre), q_suf=(suf_q, q_suf),
+            k_suf=(suf_kv, k_suf), v_suf=(suf_kv, v_suf), do_pre=(pre_q, do_pre), do_suf=(suf_q, do_suf),
+            dq_pre=(pre_q, out[0]), dk_pre=(pre_kv, out[1]), dv_pre=(pre_kv, out[2]), dq_suf=(suf_q, out[3]),
+            dk_suf=(suf_kv, out[4]), dv_suf=(suf_kv, out[5]))
+    _expect(dev, None, log_decay=((hkv,), log_decay))
+    _grouping(dev, cu_prefix=(ng + 1, cu_prefix), cu_suffix=(ns + 1, cu_suffix), group_sizes=(ng, group_sizes))
+    _workspace(workspace, dev)
+    with torch.cuda.device(dev):
+        st = lib().pg_linear_bwd(
+            _dtype_code(torch, dt), ng, ns, tp, ts, _ptr(cu_prefix), _ptr(cu_suffix), _ptr(group_sizes), hq, hkv, d,
+            float(scale), _ptr(log_decay), _ptr(q_pre), _ptr(k_pre), _ptr(v_pre), _ptr(q_suf), _ptr(k_suf), _ptr(v_suf),
+            _ptr(do_pre), _ptr(do_suf), *[_ptr(t) for t in out], _ptr(workspace), workspace.numel(),
+            _stream(torch, dev))
+    _check(st)
+    return tuple(out)
+
+
+def linear_step(q, k, v, state, log_decay, scale, out=None):
+    """One token for each of n sequences (pg_linear_step): q [n, h_q, d], k, v [n, h_kv, d], ``state`` float32
+    [n, h_kv, d, d]. ``out`` = (o, state_out), state_out may be ``state``; by default o is new and the state is updated
+    in place. Returns (o, state_out)."""
+    import torch
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k must be [sequences, heads, head_dim]")
+    (n, hq, d), hkv, dev = q.shape, k.shape[1], q.device
+    if out is None:
+        out = (torch.empty_like(q), state)
+    _expect(dev, q.dtype, q=((n, hq, d), q), k=((n, hkv, d), k), v=((n, hkv, d), v), o=((n, hq, d), out[0]))
+    _expect(dev, None, log_decay=((hkv,), log_decay), state=((n, hkv, d, d), state), state_out=((n, hkv, d, d), out[1]))
+    with torch.cuda.device(dev):
+        st = lib().pg_linear_step(_dtype_code(torch, q.dtype), n, hq, hkv, d, float(scale), _ptr(log_decay), _ptr(q),
+                                  _ptr(k), _ptr(v), _ptr(state), _ptr(out[0]), _ptr(out[1]), _stream(torch, dev))
+    _check(st)
+    return tuple(out)
+
+
+def token_logprobs_workspace_bytes(n_groups, n_suffixes, total_suffix, vocab) -> int:
+    return int(lib().pg_token_logprobs_workspace_size(n_groups, n_suffixes, total_suffix, vocab))
+
+
+def _logit_rows(device, dtype, **tensors):
+    """Logits: [rows, vocab] with contiguous rows at any stride >= vocab."""
+    for name, (shape, t) in tensors.items():
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        if t.dtype != dtype:
+            raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+        if t.device != device:
+            raise ValueError(f"{name} is on {t.device}, expected {device}")
+        if shape[1] > 1 and t.stride(1) != 1 or shape[0] > 1 and t.stride(0) < shape[1]:
+            raise ValueError(f"{name} must have contiguous rows that do not overlap")
+
+
+def _row_stride(t):
+    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+
+def _logprob_args(logits_last, logits_suf, tokens, cu_prefix, cu_suffix, group_sizes):
+    import torch
+    if logits_last.dim() != 2 or logits_suf.dim() != 2:
+        raise ValueError("logits must be [rows, vocab]")
+    ng, ns, (ts, vocab), dev = group_sizes.numel(), cu_suffix.numel() - 1, logits_suf.shape, logits_suf.device
+    _logit_rows(dev, logits_suf.dtype, logits_last=((ng, vocab), logits_last), logits_suf=((ts, vocab), logits_suf))
+    if tokens.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"tokens have dtype {tokens.dtype}, expected int32 or int64")
+    _expect(dev, tokens.dtype, tokens=((ts,), tokens))
+    _grouping(dev, cu_prefix=(ng + 1, cu_prefix), cu_suffix=(ns + 1, cu_suffix), group_sizes=(ng, group_sizes))
+    return ng, ns, ts, vocab, dev
+
+
+def token_logprobs(logits_last, logits_suf, tokens, cu_prefix, cu_suffix, group_sizes, total_prefix, temperature=1.0,
+                   entropy=False, out=None, workspace=None):
+    """Log-probabilities of the responses' tokens (pg_token_logprobs): logits_last [n_groups, vocab] of each group's
+    last prefix row, logits_suf [total_suffix, vocab] (rows at any stride), tokens [total_suffix] int32 or int64.
+    Returns (logp, lse), with ``entropy`` also the entropies, all [total_suffix] float32."""
+    import torch
+    ng, ns, ts, vocab, dev = _logprob_args(logits_last, logits_suf, tokens, cu_prefix, cu_suffix, group_sizes)
+    if out is None:
+        out = tuple(torch.empty(ts, device=dev) for _ in range(3 if entropy else 2))
+    if workspace is None:
+        workspace = torch.empty(token_logprobs_workspace_bytes(ng, ns, ts, vocab), device=dev, dtype=torch.uint8)
+    _expect(dev, None, **{n: ((ts,), t) for n, t in zip(("logp", "lse", "entropy"), out[:3 if entropy else 2])})
+    _workspace(workspace, dev)
+    with torch.cuda.device(dev):
+        st = lib().pg_token_logprobs(
+            _dtype_code(torch, logits_suf.dtype), tokens.element_size(), ng, ns, int(total_prefix), ts,
+            _ptr(cu_prefix), _ptr(cu_suffix), _ptr(group_sizes), vocab, float(temperature), _ptr(logits_last),
+            _row_stride(logits_last), _ptr(logits_suf), _row_stride(logits_suf), _ptr(tokens), _ptr(out[0]),
+            _ptr(out[1]), _ptr(out[2]) if entropy else None, _ptr(workspace), workspace.numel(), _stream(torch, dev))
+    _check(st)
+    return tuple(out[:3 if entropy else 2])
+
+
+def token_logprobs_bwd(logits_last, logits_suf, tokens, lse, dlogp, cu_prefix, cu_suffix, group_sizes, total_prefix,
+                       temperature=1.0, out=None, workspace=None):
+    """Gradient of token_logprobs (pg_token_logprobs_bwd): ``lse`` as the forward returned it, ``dlogp``
+    [total_suffix] float32. ``out`` = (dlogits_last, dlogits_suf), which may be the logits themselves. Returns both."""
+    import torch
+    ng, ns, ts, vocab, dev = _logprob_args(logits_last, logits_suf, tokens, cu_prefix, cu_suffix, group_sizes)
+    dt = logits_suf.dtype
+    if out is None:
+        out = (torch.empty((ng, vocab), device=dev, dtype=dt), torch.empty((ts, vocab), device=dev, dtype=dt))
+    if workspace is None:
+        workspace = torch.empty(token_logprobs_workspace_bytes(ng, ns, ts, vocab), device=dev, dtype=torch.uint8)
+    _expect(dev, None, lse=((ts,), lse), dlogp=((ts,), dlogp))
+    _logit_rows(dev, dt, dlogits_last=((ng, vocab), out[0]), dlogits_suf=((ts, vocab), out[1]))
+    _workspace(workspace, dev)
+    with torch.cuda.device(dev):
+        st = lib().pg_token_logprobs_bwd(
+            _dtype_code(torch, dt), tokens.element_size(), ng, ns, int(total_prefix), ts, _ptr(cu_prefix),
+            _ptr(cu_suffix), _ptr(group_sizes), vocab, float(temperature), _ptr(logits_last), _row_stride(logits_last),
+            _ptr(logits_suf), _row_stride(logits_suf), _ptr(tokens), _ptr(lse), _ptr(dlogp), _ptr(out[0]),
+            _row_stride(out[0]), _ptr(out[1]), _row_stride(out[1]), _ptr(workspace), workspace.numel(),
+            _stream(torch, dev))
+    _check(st)
+    return tuple(out)
+
+
+def policy_loss_workspace_bytes(n_groups, n_suffixes, total_suffix) -> int:
+    return int(lib().pg_policy_loss_workspace_size(n_groups, n_suffixes, total_suffix))
+
+
+AVERAGES = {"group": 0, "token": 1}
+
+
+def policy_loss(logp, advantages, cu_suffix, group_sizes, logp_old=None, logp_ref=None, mask=None, clip=(0.2, 0.2),
+                beta=0.0, average="group", grad_scale=1.0, out=None, workspace=None):
+    """The clipped policy loss with a KL term and its gradient (pg_policy_loss). logp, logp_old, logp_ref
+    [total_suffix] float32, advantages [n_suffixes] float32, mask [total_suffix] bool or uint8. Returns
+    (stats [4]: loss, policy term, KL term, share clipped; dlogp [total_suffix])."""
+    import torch
+    ng, ns, ts, dev = group_sizes.numel(), cu_suffix.numel() - 1, logp.numel(), logp.device
+    if average not in AVERAGES:
+        raise ValueError(f"average must be one of {sorted(AVERAGES)}, got {average!r}")
+    if out is None:
+        out = (torch.empty(4, device=dev), torch.empty(ts, device=dev))
+    if workspace is None:
+        workspace = torch.empty(policy_loss_workspace_bytes(ng, ns, ts), device=dev, dtype=torch.uint8)
+    f32 = {"logp": ((ts,), logp), "advantages": ((ns,), advantages), "stats": ((4,), out[0]), "dlogp": ((ts,), out[1])}
+    if logp_old is not None:
+        f32["logp_old"] = ((ts,), logp_old)
+    if logp_ref is not None:
+        f32["logp_ref"] = ((ts,), logp_ref)
+    _expect(dev, None, **f32)
+    if mask is not None:
+        if mask.dtype not in (torch.bool, torch.uint8):
+            raise TypeError(f"mask has dtype {mask.dtype}, expected bool or uint8")
+        _expect(dev, mask.dtype, mask=((ts,), mask))
+    _grouping(dev, cu_suffix=(ns + 1, cu_suffix), group_sizes=(ng, group_sizes))
+    _workspace(workspace, dev)
+    with torch.cuda.device(dev):
+        st = lib().pg_policy_loss(
+            AVERAGES[average], ng, ns, ts, _ptr(cu_suffix), _ptr(group_sizes), float(clip[0]), float(clip[1]),
+            float(beta), float(grad_scale), _ptr(logp), _ptr(logp_old), _ptr(logp_ref), _ptr(advantages), _ptr(mask),
+            _ptr(out[0]), _ptr(out[1]), _ptr(workspace), workspace.numel(), _stream(torch, dev))
+    _check(st)
+    return tuple(out)
 
 
 def to_device(prob, device="cuda"):

@@ -1,0 +1,581 @@
+// Log-probabilities of the responses' tokens from the logits, their gradient, and the clipped policy loss.
+//
+// In the grouped layout response row j of a member predicts token j + 1 of it, and the last prefix row of a group
+// predicts the first token of every one of its members: one softmax with as many targets as the group has members,
+// whose gradient sums over them (Lemma 1's sum over the copies of the prefix, for its last row).
+//
+// Both logits kernels read a row once, one workgroup a row, 16 bytes a lane and load, and are bound by that traffic:
+// forward with a running maximum and sum (softmax statistics and the entropy's sum in fp32), backward from the saved
+// log-sum-exp. Rows start at any alignment the element type has; a row's first elements up to a 16-byte boundary and
+// its last ones are taken one by one.
+#pragma once
+#include "pg_common.hpp"
+#include "pg_plan.hpp"
+
+namespace pg {
+
+struct LogprobArgs {
+  const void *last, *suf;  // logits [n_groups, vocab], [total_suffix, vocab]
+  void *d_last, *d_suf;
+  long ld_last, ld_suf, ldd_last, ldd_suf;  // elements between rows
+  const void* tokens;                       // [total_suffix], int32 or int64
+  int tok64;
+  float *logp, *lse, *entropy;
+  const float* dlogp;
+  const int *cu_p, *cu_s;
+  const PlanHeader* hdr;
+  const GroupInfoEx* ginfo;
+  int ng, ns, ts, vocab;
+  float inv_temp;
+};
+
+// Largest index i in [0, n) with a[i] <= x (a nondecreasing, a[0] <= x), by a whole wave: 64 entries a step.
+__device__ __forceinline__ int wave_upper_index(const int* __restrict__ a, int n, int x) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, len = n;
+  while (len > 1) {
+    const int step = (len + 63) / 64;
+    const int i = lo + lane * step;
+    const bool le = lane * step < len && a[i] <= x;  // true for a prefix of the lanes, lane 0 among them
+    const int cnt = __popcll(__ballot(le));
+    const int first = (cnt - 1) * step;
+    lo += first;
+    len = min(step, len - first);
+  }
+  return uniform(lo);
+}
+
+// The token at response row r, or -1 where it is outside [0, vocab).
+__device__ __forceinline__ int token_at(const LogprobArgs& a, int r) {
+  const long t = a.tok64 ? ((const long long*)a.tokens)[r] : (long)((const int*)a.tokens)[r];
+  return t >= 0 && t < a.vocab ? (int)t : -1;
+}
+
+// Elements of 16 bytes as floats.
+template <typename T>
+struct Vec16;
+template <>
+struct Vec16<bf16> {
+  static constexpr int kN = 8;
+  __device__ __forceinline__ static void unpack(const uint4& u, float (&x)[8]) {
+    const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ static uint4 pack(const float (&x)[8]) {
+    bf16x8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (bf16)x[i];
+    return __builtin_bit_cast(uint4, v);
+  }
+};
+template <>
+struct Vec16<float> {
+  static constexpr int kN = 4;
+  __device__ __forceinline__ static void unpack(const uint4& u, float (&x)[4]) {
+    x[0] = __uint_as_float(u.x);
+    x[1] = __uint_as_float(u.y);
+    x[2] = __uint_as_float(u.z);
+    x[3] = __uint_as_float(u.w);
+  }
+  __device__ __forceinline__ static uint4 pack(const float (&x)[4]) {
+    return uint4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+  }
+};
+
+// Elements before the first 16-byte boundary of a row (a row of fewer elements is all head).
+template <typename T>
+__device__ __forceinline__ int row_head(const T* p, int n) {
+  const int h = (int)((16 - ((uintptr_t)p & 15)) & 15) / (int)sizeof(T);
+  return h < n ? h : n;
+}
+
+// Running softmax statistics in base 2: m the largest x seen, s = sum 2^(c (x - m)), w = sum 2^(c (x - m)) c (x - m).
+struct SoftStat {
+  float m, s, w;
+};
+constexpr float kFarBelow = -1e30f;  // a finite stand-in for c (x - m) of x = -inf, whose term is 0
+constexpr float kFarOut = 1e36f;     // c x might overflow from here on (rows masked with the type's lowest value)
+
+template <bool ENT, int N>
+__device__ __forceinline__ void soft_add(SoftStat& a, const float (&x)[N], float c) {
+  float mx = x[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) mx = fmaxf(mx, x[i]);
+  if (mx > a.m) {
+    const float z = fmaxf(c * (a.m - mx), kFarBelow), f = fast_exp2(z);
+    if (ENT) a.w = f * (a.w + a.s * z);
+    a.s *= f;
+    a.m = mx;
+  }
+  if (fabsf(a.m) < kFarOut) {
+    const float off = -c * a.m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float z = fmaf(c, x[i], off), e = fast_exp2(z);
+      a.s += e;
+      if (ENT) a.w += e * fmaxf(z, kFarBelow);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (x[i] == -INFINITY) continue;
+      const float z = c * (x[i] - a.m), e = fast_exp2(z);
+      a.s += e;
+      if (ENT) a.w += e * fmaxf(z, kFarBelow);
+    }
+  }
+}
+
+__device__ __forceinline__ SoftStat soft_join(const SoftStat& a, const SoftStat& b, float c) {
+  SoftStat r;
+  r.m = fmaxf(a.m, b.m);
+  const float za = a.m == r.m ? 0.f : fmaxf(c * (a.m - r.m), kFarBelow);
+  const float zb = b.m == r.m ? 0.f : fmaxf(c * (b.m - r.m), kFarBelow);
+  const float fa = fast_exp2(za), fb = fast_exp2(zb);
+  r.s = a.s * fa + b.s * fb;
+  r.w = fa * (a.w + a.s * za) + fb * (b.w + b.s * zb);
+  return r;
+}
+
+// Row b of the logits: the groups' last prefix rows, then the response rows. `targets`: the response rows
+// [first of each member m0 .. m1), or the one row `target`; none when target < 0 and m0 == m1.
+struct LogitRow {
+  int group, target, m0, m1;
+};
+__device__ __forceinline__ LogitRow logit_row(const LogprobArgs& a, long b) {
+  LogitRow r{-1, -1, 0, 0};
+  if (b < a.ng) {
+    r.group = (int)b;
+    const GroupInfoEx gi = a.ginfo[b];
+    if (gi.p1 > gi.p0) {  // an empty prefix has no row that predicts
+      r.m0 = gi.m0;
+      r.m1 = gi.m1;
+    }
+  } else {
+    const int row = (int)(b - a.ng), m = wave_upper_index(a.cu_s, a.ns, row);
+    if (row + 1 < a.cu_s[m + 1]) r.target = row + 1;
+  }
+  return r;
+}
+
+// The statistics of a whole row, by the workgroup; every thread gets them. part: one entry for each wave.
+template <typename T, int NT, bool ENT>
+__device__ __forceinline__ SoftStat row_stats(const T* x, int vocab, float c, SoftStat* part) {
+  using V = Vec16<T>;
+  constexpr int kUnroll = 4;
+  const int t = threadIdx.x;
+  SoftStat st{-INFINITY, 0.f, 0.f};
+  const int head = row_head(x, vocab), nv = (vocab - head) / V::kN, tail = head + nv * V::kN;
+  if (t < head) {
+    const float v[1] = {(float)x[t]};
+    soft_add<ENT>(st, v, c);
+  }
+  if (t < vocab - tail) {
+    const float v[1] = {(float)x[tail + t]};
+    soft_add<ENT>(st, v, c);
+  }
+  const uint4* xv = (const uint4*)(x + head);
+  int i = t;
+  for (; i + (kUnroll - 1) * NT < nv; i += kUnroll * NT) {
+    uint4 u[kUnroll];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) u[k] = xv[i + k * NT];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      float v[V::kN];
+      V::unpack(u[k], v);
+      soft_add<ENT>(st, v, c);
+    }
+  }
+  for (; i < nv; i += NT) {
+    float v[V::kN];
+    V::unpack(xv[i], v);
+    soft_add<ENT>(st, v, c);
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    SoftStat o;
+    o.m = __shfl_xor(st.m, off);
+    o.s = __shfl_xor(st.s, off);
+    o.w = __shfl_xor(st.w, off);
+    st = soft_join(st, o, c);
+  }
+  if ((t & 63) == 0) part[t >> 6] = st;
+  __syncthreads();
+  st = part[0];
+#pragma unroll
+  for (int k = 1; k < NT / 64; ++k) st = soft_join(st, part[k], c);
+  __syncthreads();
+  return st;
+}
+
+template <typename T, int NT, bool ENT>
+__global__ void __launch_bounds__(NT) logprob_kernel(const LogprobArgs a) {
+  __shared__ SoftStat part[NT / 64];
+  if (a.hdr->error) return;
+  const int t = threadIdx.x;
+  const float c = a.inv_temp * kLog2e;
+  for (long b = blockIdx.x; b < (long)a.ng + a.ts; b += gridDim.x) {
+    const LogitRow row = logit_row(a, b);
+    if (row.group >= 0 && row.m0 == row.m1) {
+      // no row predicts the first tokens of this group's members
+      const GroupInfoEx gi = a.ginfo[row.group];
+      for (int m = gi.m0 + t; m < gi.m1; m += NT) {
+        const int r = a.cu_s[m];
+        if (r == a.cu_s[m + 1]) continue;
+        a.logp[r] = 0.f;
+        a.lse[r] = -INFINITY;
+        if (ENT) a.entropy[r] = 0.f;
+      }
+      continue;
+    }
+    if (row.group < 0 && row.target < 0) continue;
+    const T* x = row.group >= 0 ? (const T*)a.last + row.group * a.ld_last : (const T*)a.suf + (b - a.ng) * a.ld_suf;
+    const SoftStat st = row_stats<T, NT, ENT>(x, a.vocab, c, part);
+    // ln sum exp(x / T), and the entropy ln s - sum p ln 2 c (x - m)
+    const bool none = st.m == -INFINITY;
+    const float ln_s = logf(st.s);
+    const float lse = none ? -INFINITY : st.m * a.inv_temp + ln_s;
+    float ent = none ? 0.f : ln_s - kLn2 * st.w / st.s;
+    if (ent < 0.f) ent = 0.f;  // by rounding only; a NaN stays
+    auto put = [&](int r) {
+      const int tok = token_at(a, r);
+      float lp = 0.f;
+      if (tok >= 0) lp = none ? -INFINITY : ((float)x[tok] - st.m) * a.inv_temp - ln_s;
+      a.logp[r] = lp;
+      a.lse[r] = lse;
+      if (ENT) a.entropy[r] = ent;
+    };
+    if (row.group < 0) {
+      if (t == 0) put(row.target);
+    } else {
+      for (int m = row.m0 + t; m < row.m1; m += NT)
+        if (a.cu_s[m + 1] > a.cu_s[m]) put(a.cu_s[m]);
+    }
+  }
+}
+
+// dlogits = (1 / T) sum over the row's targets of dlogp (onehot - softmax). A row without a target, or whose targets
+// all have dlogp = 0 or a token outside the vocabulary, or with no finite logit, gets zeros and is not read.
+// A group row marks its targets' 16-byte pieces in an LDS bitmap (a hash: false hits only cost time) and, where a
+// piece is marked, walks the members in order.
+constexpr int kMarkBits = 8192;
+
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT) logprob_bwd_kernel(const LogprobArgs a) {
+  using V = Vec16<T>;
+  constexpr int kUnroll = 4;
+  __shared__ unsigned mark[kMarkBits / 32];
+  __shared__ float sum_part[NT / 64], lse_part[NT / 64];
+  __shared__ int any_part[NT / 64];
+  __shared__ SoftStat stat_part[NT / 64];
+  if (a.hdr->error) return;
+  const int t = threadIdx.x;
+  const float c = a.inv_temp * kLog2e;
+  for (long b = blockIdx.x; b < (long)a.ng + a.ts; b += gridDim.x) {
+    const LogitRow row = logit_row(a, b);
+    const bool grp = row.group >= 0;
+    const T* x = grp ? (const T*)a.last + row.group * a.ld_last : (const T*)a.suf + (b - a.ng) * a.ld_suf;
+    T* dx = grp ? (T*)a.d_last + row.group * a.ldd_last : (T*)a.d_suf + (b - a.ng) * a.ldd_suf;
+    // the gradient's head follows dx's alignment; x may have another one, then it is read element by element
+    const int head = row_head(dx, a.vocab), nv = (a.vocab - head) / V::kN, tail = head + nv * V::kN;
+    const bool same = (((uintptr_t)x ^ (uintptr_t)dx) & 15) == 0;
+    float total = 0.f, lse = -INFINITY, d1 = 0.f;
+    int tok1 = -1, any = 0;
+    if (grp) {
+      for (int i = t; i < kMarkBits / 32; i += NT) mark[i] = 0;
+      __syncthreads();
+      float sum = 0.f, l = -INFINITY;
+      for (int m = row.m0 + t; m < row.m1; m += NT) {
+        const int r = a.cu_s[m];
+        if (r == a.cu_s[m + 1]) continue;
+        const int tok = token_at(a, r);
+        l = a.lse[r];  // the same for every member: the row's own
+        const float d = a.dlogp[r];
+        if (tok < 0 || d == 0.f) continue;
+        any = 1;
+        sum += d;
+        if (tok >= head && tok < tail) {
+          const int p = ((tok - head) / V::kN) % kMarkBits;
+          atomicOr(&mark[p / 32], 1u << (p % 32));
+        }
+      }
+      // a fixed order: the members of a lane, the lanes of a wave, the waves
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) {
+        sum += __shfl_xor(sum, off);
+        const float o = __shfl_xor(l, off);
+        l = l == -INFINITY ? o : l;
+        any |= __shfl_xor(any, off);
+      }
+      if ((t & 63) == 0) {
+        sum_part[t >> 6] = sum;
+        lse_part[t >> 6] = l;
+        any_part[t >> 6] = any;
+      }
+      __syncthreads();
+      any = 0;
+#pragma unroll
+      for (int k = 0; k < NT / 64; ++k) {
+        total += sum_part[k];
+        any |= any_part[k];
+        if (lse == -INFINITY) lse = lse_part[k];
+      }
+    } else if (row.target >= 0) {
+      tok1 = token_at(a, row.target);
+      d1 = a.dlogp[row.target];
+      lse = a.lse[row.target];
+      if (tok1 >= 0 && d1 != 0.f) {
+        any = 1;
+        total = d1;
+      } else {
+        tok1 = -1;
+      }
+    }
+    // what a member whose first token is `tok` adds: the members in order
+    auto hits = [&](int e0, int n, float* add) {
+      for (int m = row.m0; m < row.m1; ++m) {
+        const int r = a.cu_s[m];
+        if (r == a.cu_s[m + 1]) continue;
+        const int tok = token_at(a, r);
+        if (tok >= e0 && tok < e0 + n) add[tok - e0] += a.dlogp[r];
+      }
+    };
+    if (lse == -INFINITY) any = 0;
+    // p = 2^(c x - lse log2 e); where the log-sum-exp is too large for that it has also lost ln s (a row masked with
+    // the type's lowest value throughout), and the statistics are taken again: p = 2^(c (x - m)) / s
+    const bool far = any && fabsf(lse) >= kFarOut;
+    float off = -lse * kLog2e, w = -total * a.inv_temp, top = 0.f;
+    if (far) {
+      const SoftStat st = row_stats<T, NT, false>(x, a.vocab, c, stat_part);
+      top = st.m;
+      off = 0.f;
+      w /= st.s;
+    }
+    auto prob = [&](float v) { return fast_exp2(far ? c * (v - top) : fmaf(c, v, off)); };
+    auto one = [&](int e) {
+      float y = 0.f;
+      if (any) {
+        float add = 0.f;
+        if (grp) hits(e, 1, &add);
+        else if (e == tok1) add = d1;
+        y = fmaf(add, a.inv_temp, prob((float)x[e]) * w);  // as vec() forms it, bit for bit
+      }
+      dx[e] = (T)y;
+    };
+    if (t < head) one(t);
+    if (t < a.vocab - tail) one(tail + t);
+    uint4* dv = (uint4*)(dx + head);
+    if (!any) {
+      for (int i = t; i < nv; i += NT) dv[i] = uint4{0, 0, 0, 0};
+    } else {
+      auto vec = [&](int i, const float (&v)[V::kN]) {
+        float y[V::kN];
+#pragma unroll
+        for (int k = 0; k < V::kN; ++k) y[k] = prob(v[k]) * w;
+        const int e0 = head + i * V::kN;
+        if (grp) {
+          const int p = i % kMarkBits;
+          if (mark[p / 32] >> (p % 32) & 1) {
+            float add[V::kN] = {};
+            hits(e0, V::kN, add);
+#pragma unroll
+            for (int k = 0; k < V::kN; ++k) y[k] = fmaf(add[k], a.inv_temp, y[k]);
+          }
+        } else if ((unsigned)(tok1 - e0) < (unsigned)V::kN) {
+#pragma unroll
+          for (int k = 0; k < V::kN; ++k)
+            if (tok1 - e0 == k) y[k] = fmaf(d1, a.inv_temp, y[k]);
+        }
+        dv[i] = V::pack(y);
+      };
+      const T* xs = x + head;
+      int i = t;
+      if (same) {
+        for (; i + (kUnroll - 1) * NT < nv; i += kUnroll * NT) {
+          uint4 u[kUnroll];
+#pragma unroll
+          for (int k = 0; k < kUnroll; ++k) u[k] = ((const uint4*)xs)[i + k * NT];
+#pragma unroll
+          for (int k = 0; k < kUnroll; ++k) {
+            float v[V::kN];
+            V::unpack(u[k], v);
+            vec(i + k * NT, v);
+          }
+        }
+      }
+      for (; i < nv; i += NT) {
+        float v[V::kN];
+        if (same) {
+          V::unpack(((const uint4*)xs)[i], v);
+        } else {
+#pragma unroll
+          for (int k = 0; k < V::kN; ++k) v[k] = (float)xs[i * V::kN + k];
+        }
+        vec(i, v);
+      }
+    }
+    __syncthreads();  // mark and the partial sums are reused by the next row
+  }
+}
+
+// ---------------------------------------------------------------- policy loss
+// Token t of member m of group g, with r = exp(lp - lp_old), A the member's advantage, x = lp_ref - lp:
+//   L_t = -min(r A, clip(r, 1 - lo, 1 + hi) A) + beta (exp(x) - x - 1),   loss = sum_t w_t L_t,
+//   dL_t / dlp = -[not clipped] r A + beta (1 - exp(x)).
+// w_t = 1 / (groups with members * members of g * kept tokens of m), or 1 / all kept tokens. The arithmetic is in
+// fp64: a batch has at most some hundred thousand tokens of 20 bytes each, so the time is launches and latency, the
+// ratio next to the clip's border is decided as the definition does, and the sums cancel.
+struct PolicyArgs {
+  const float *logp, *logp_old, *logp_ref, *adv;
+  const unsigned char* mask;
+  const int *cu_s, *gsz;
+  float *stats, *dlogp;
+  PlanHeader* hdr;
+  double* member_w;  // [n_suffixes]: 1 / (groups * members) of each member
+  int* count;        // [n_suffixes + 1]: kept tokens of each member, and of all
+  double* part;      // [blocks, 4]
+  unsigned* done;
+  int ng, ns, ts, by_token, blocks;
+  double cut_lo, cut_hi, beta, grad_scale;
+};
+constexpr int kPolicyThreads = 1024, kPolicyTok = 256;
+
+// Checks and per-member weights; one block.
+__global__ void __launch_bounds__(kPolicyThreads) policy_plan_kernel(const PolicyArgs a) {
+  __shared__ long long tmp[kPolicyThreads];
+  __shared__ long long members;
+  __shared__ int bad, groups;
+  const int t = threadIdx.x;
+  if (t == 0) {
+    members = 0;
+    bad = 0;
+    groups = 0;
+  }
+  __syncthreads();
+  int b = 0;
+  for (int m = t; m <= a.ns; m += kPolicyThreads) {
+    const int v = a.cu_s[m];
+    if ((m == 0 && v != 0) || (m == a.ns && v != a.ts) || (m > 0 && v < a.cu_s[m - 1])) b = 1;
+  }
+  int full = 0;
+  for (int g = t; g < a.ng; g += kPolicyThreads) {
+    const int v = a.gsz[g];
+    if (v < 0 || v > a.ns) b = 1;
+    full += v > 0;
+  }
+  if (b) atomicOr(&bad, 1);
+  if (full) atomicAdd(&groups, full);
+  __syncthreads();
+  for (int base = 0; base < a.ng && !bad; base += kPolicyThreads) {
+    const int g = base + t;
+    const long long v = g < a.ng ? a.gsz[g] : 0;
+    const long long end = members + block_inclusive_scan<kPolicyThreads>(v, tmp);
+    if (g < a.ng && end <= a.ns)
+      for (long long m = end - v; m < end; ++m) a.member_w[m] = 1.0 / ((double)groups * (double)v);
+    __syncthreads();
+    if (t == kPolicyThreads - 1) members = end;
+    __syncthreads();
+  }
+  for (int m = t; m <= a.ns; m += kPolicyThreads)
+    a.count[m] = a.mask || bad ? 0 : m < a.ns ? a.cu_s[m + 1] - a.cu_s[m] : a.ts;
+  if (t == 0) {
+    a.hdr->error = bad || members != a.ns;
+    *a.done = 0;
+  }
+}
+
+// Kept tokens of each member (whole numbers: their order does not matter).
+__global__ void __launch_bounds__(kPolicyTok) policy_count_kernel(const PolicyArgs a) {
+  if (a.hdr->error) return;
+  const long i = (long)blockIdx.x * kPolicyTok + threadIdx.x;
+  const bool on = i < a.ts && a.mask[i];
+  const int m = i < a.ts ? upper_index(a.cu_s, 0, a.ns, (int)i) : -1;
+  const int m0 = uniform(m);
+  const unsigned long long all = __ballot(on);
+  if ((threadIdx.x & 63) == 0 && all) atomicAdd(&a.count[a.ns], __popcll(all));
+  if (__all(m == m0 || m < 0)) {
+    if ((threadIdx.x & 63) == 0 && all) atomicAdd(&a.count[m0], __popcll(all));
+  } else if (on) {
+    atomicAdd(&a.count[m], 1);
+  }
+}
+
+struct PolicySums {
+  double v[4];
+};
+__device__ __forceinline__ void policy_token(const PolicyArgs& a, int i, int m, double w, PolicySums& s) {
+  const bool on = !a.mask || a.mask[i];
+  double grad = 0.0;
+  if (on) {
+    const double lp = a.logp[i], adv = a.adv[m];
+    const double lr = a.logp_old ? lp - (double)a.logp_old[i] : 0.0;
+    const bool cut = (adv > 0.0 && lr > a.cut_hi) || (adv < 0.0 && lr < a.cut_lo);
+    const double r = exp(cut ? (adv > 0.0 ? a.cut_hi : a.cut_lo) : lr);
+    const double ra = adv == 0.0 ? 0.0 : r * adv;
+    double kl = 0.0;
+    grad = cut ? 0.0 : -ra;
+    if (a.logp_ref) {
+      const double x = (double)a.logp_ref[i] - lp, em = expm1(x);
+      kl = em - x;
+      if (a.beta != 0.0) grad -= a.beta * em;
+    }
+    s.v[0] += w * ((a.beta != 0.0 ? a.beta * kl : 0.0) - ra);
+    s.v[1] -= w * ra;
+    s.v[2] += w * kl;
+    s.v[3] += cut ? w : 0.0;
+    grad *= w * a.grad_scale;
+  }
+  if (a.dlogp) a.dlogp[i] = (float)grad;
+}
+
+__device__ __forceinline__ double policy_weight(const PolicyArgs& a, int m) {
+  const int n = a.count[a.by_token ? a.ns : m];
+  return n == 0 ? 0.0 : a.by_token ? 1.0 / n : a.member_w[m] / n;
+}
+
+template <int NT>
+__device__ __forceinline__ void block_sum4(PolicySums& s, double (*tmp)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) s.v[k] += __shfl_xor(s.v[k], off);
+    if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6][k] = s.v[k];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    double x = 0.0;
+    for (int w = 0; w < NT / 64; ++w) x += tmp[w][k];
+    s.v[k] = x;
+  }
+}
+
+__global__ void __launch_bounds__(kPolicyTok) policy_loss_kernel(const PolicyArgs a) {
+  __shared__ double tmp[kPolicyTok / 64][4];
+  if (a.hdr->error) return;
+  PolicySums s{{0.0, 0.0, 0.0, 0.0}};
+  for (long i = (long)blockIdx.x * kPolicyTok + threadIdx.x; i < a.ts; i += (long)gridDim.x * kPolicyTok) {
+    const int m = upper_index(a.cu_s, 0, a.ns, (int)i);
+    policy_token(a, (int)i, m, policy_weight(a, m), s);
+  }
+  block_sum4<kPolicyTok>(s, tmp);
+  if (threadIdx.x < 4) a.part[4 * blockIdx.x + threadIdx.x] = s.v[threadIdx.x];
+}
+
+// The blocks' sums, in block order.
+__global__ void __launch_bounds__(64) policy_sum_kernel(const PolicyArgs a) {
+  if (a.hdr->error) return;
+  double x = 0.0;
+  const int k = threadIdx.x & 3;
+  for (int b = threadIdx.x >> 2; b < a.blocks; b += 16) x += a.part[4 * b + k];
+#pragma unroll
+  for (int off = 32; off >= 4; off >>= 1) x += __shfl_xor(x, off);
+  if (threadIdx.x < 4) a.stats[threadIdx.x] = (float)x;
+}
+
+}  // namespace pg

@@ -1,0 +1,151 @@
+"""Refusals of linear attention, the token log-probabilities and the policy loss: in the C ABI and in the binding, before
+anything reaches a device. CPU only."""
+import ctypes
+
+import pytest
+
+from paper_2506_05433_amd import binding
+
+torch = pytest.importorskip("torch")
+
+OK, EINVAL, EUNSUPPORTED, EWORKSPACE = 0, 1, 2, 3
+P = lambda v: ctypes.c_void_p(v) if v else None  # noqa: E731
+
+
+def _linear(which, **over):
+    a = dict(dtype=0, ng=1, ns=2, tp=8, ts=6, cu_p=64, cu_s=64, gsz=64, h_q=4, h_kv=2, d=128, scale=0.125, decay=64,
+             pre=64, suf=64, state_in=0, states=0, ws=256, ws_bytes=1 << 40)
+    a.update(over)
+    head = [a["dtype"], a["ng"], a["ns"], a["tp"], a["ts"], P(a["cu_p"]), P(a["cu_s"]), P(a["gsz"]), a["h_q"], a["h_kv"],
+            a["d"], a["scale"], P(a["decay"])]
+    if which == "fwd":
+        tens = [P(a["pre"])] * 3 + [P(a["suf"])] * 3 + [P(a["state_in"]), P(a["pre"]), P(a["suf"]), P(a["states"]), P(a["states"])]
+        return binding.lib().pg_linear_fwd(*head, *tens, P(a["ws"]), a["ws_bytes"], None)
+    tens = [P(a["pre"])] * 3 + [P(a["suf"])] * 3 + [P(a["pre"]), P(a["suf"])] + [P(a["pre"])] * 3 + [P(a["suf"])] * 3
+    return binding.lib().pg_linear_bwd(*head, *tens, P(a["ws"]), a["ws_bytes"], None)
+
+
+@pytest.mark.parametrize("which", ["fwd", "bwd"])
+@pytest.mark.parametrize("over,status", [
+    (dict(dtype=2), EUNSUPPORTED), (dict(ng=-1), EINVAL), (dict(ts=-1), EINVAL), (dict(ng=0, ns=0, ts=0), EINVAL),
+    (dict(ns=0), EINVAL), (dict(h_q=5), EINVAL), (dict(h_kv=0), EINVAL), (dict(d=96), EUNSUPPORTED),
+    (dict(h_q=1024, h_kv=8), EUNSUPPORTED), (dict(scale=0.0), EINVAL), (dict(scale=float("nan")), EINVAL),
+    (dict(cu_p=0), EINVAL), (dict(cu_s=0), EINVAL), (dict(gsz=0), EINVAL), (dict(decay=0), EINVAL), (dict(pre=0), EINVAL),
+    (dict(suf=0), EINVAL), (dict(pre=66), EINVAL), (dict(suf=72), EINVAL), (dict(ws=260), EINVAL),
+    (dict(ws=0), EWORKSPACE), (dict(ws_bytes=1000), EWORKSPACE), (dict(tp=0x7fffffff), EUNSUPPORTED),
+    (dict(ns=20_000_000), EUNSUPPORTED),
+])
+def test_linear_arguments(which, over, status):
+    assert _linear(which, **over) == status, binding.lib().pg_last_error()
+    assert binding.lib().pg_last_error()
+
+
+def test_linear_state_pointers_must_be_aligned():
+    assert _linear("fwd", state_in=68) == EINVAL and _linear("fwd", states=72) == EINVAL
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(dtype=3), EUNSUPPORTED), (dict(n=-1), EINVAL), (dict(h_q=3), EINVAL), (dict(d=32), EUNSUPPORTED),
+    (dict(scale=float("inf")), EINVAL), (dict(ptr=0), EINVAL), (dict(decay=0), EINVAL), (dict(ptr=72), EINVAL),
+])
+def test_linear_step_arguments(over, status):
+    a = dict(dtype=0, n=3, h_q=4, h_kv=2, d=64, scale=1.0, decay=64, ptr=64)
+    a.update(over)
+    st = binding.lib().pg_linear_step(a["dtype"], a["n"], a["h_q"], a["h_kv"], a["d"], a["scale"], P(a["decay"]),
+                                      *[P(a["ptr"])] * 6, None)
+    assert st == status, binding.lib().pg_last_error()
+
+
+def _logprobs(which, **over):
+    a = dict(dtype=0, tb=8, ng=1, ns=2, tp=8, ts=6, cu_p=64, cu_s=64, gsz=64, vocab=10, temp=1.0, last=64, suf=64, ld_last=10,
+             ld_suf=12, dl=128, ds=128, ldd_last=10, ldd_suf=10, tok=64, f=64, ws=64, ws_bytes=1 << 40)
+    a.update(over)
+    head = [a["dtype"], a["tb"], a["ng"], a["ns"], a["tp"], a["ts"], P(a["cu_p"]), P(a["cu_s"]), P(a["gsz"]), a["vocab"], a["temp"],
+            P(a["last"]), a["ld_last"], P(a["suf"]), a["ld_suf"], P(a["tok"]), P(a["f"]), P(a["f"])]
+    if which == "fwd":
+        return binding.lib().pg_token_logprobs(*head, None, P(a["ws"]), a["ws_bytes"], None)
+    return binding.lib().pg_token_logprobs_bwd(*head, P(a["dl"]), a["ldd_last"], P(a["ds"]), a["ldd_suf"], P(a["ws"]), a["ws_bytes"], None)
+
+
+@pytest.mark.parametrize("which", ["fwd", "bwd"])
+@pytest.mark.parametrize("over,status", [
+    (dict(dtype=9), EUNSUPPORTED), (dict(tb=2), EUNSUPPORTED), (dict(vocab=0), EINVAL), (dict(temp=0.0), EINVAL),
+    (dict(temp=float("nan")), EINVAL), (dict(temp=1e-42), EINVAL), (dict(ld_last=9), EINVAL), (dict(ld_suf=9), EINVAL),
+    (dict(last=0), EINVAL), (dict(suf=0), EINVAL), (dict(tok=0), EINVAL), (dict(f=0), EINVAL), (dict(suf=65), EINVAL),
+    (dict(dtype=1, suf=66), EINVAL), (dict(tok=68), EINVAL), (dict(ng=-1), EINVAL), (dict(ns=0), EINVAL),
+    (dict(gsz=0), EINVAL), (dict(ws=0), EWORKSPACE), (dict(ws_bytes=10), EWORKSPACE),
+])
+def test_logprob_arguments(which, over, status):
+    assert _logprobs(which, **over) == status, binding.lib().pg_last_error()
+
+
+@pytest.mark.parametrize("over", [dict(ldd_last=9), dict(ldd_suf=9), dict(dl=0), dict(ds=0), dict(ds=129), dict(ds=64)])
+def test_logprob_gradient_arguments(over):
+    assert _logprobs("bwd", **over) == EINVAL, binding.lib().pg_last_error()
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(avg=2), EINVAL), (dict(lo=-0.1), EINVAL), (dict(lo=1.5), EINVAL), (dict(hi=-1.0), EINVAL),
+    (dict(hi=float("inf")), EINVAL), (dict(lo=float("nan")), EINVAL), (dict(beta=float("nan")), EINVAL), (dict(ref=0), EINVAL),
+    (dict(scale=float("inf")), EINVAL), (dict(stats=0), EINVAL), (dict(logp=0), EINVAL), (dict(adv=0), EINVAL),
+    (dict(ng=-1), EINVAL), (dict(ns=0), EINVAL), (dict(cu_s=0), EINVAL), (dict(ws=0), EWORKSPACE), (dict(ws_bytes=99), EWORKSPACE),
+])
+def test_policy_arguments(over, status):
+    a = dict(avg=0, ng=1, ns=2, ts=6, cu_s=64, gsz=64, lo=0.2, hi=0.2, beta=0.1, scale=1.0, logp=64, old=64, ref=64, adv=64, mask=0,
+             stats=64, dlogp=64, ws=64, ws_bytes=1 << 40)
+    a.update(over)
+    st = binding.lib().pg_policy_loss(a["avg"], a["ng"], a["ns"], a["ts"], P(a["cu_s"]), P(a["gsz"]), a["lo"], a["hi"], a["beta"],
+                                      a["scale"], P(a["logp"]), P(a["old"]), P(a["ref"]), P(a["adv"]), P(a["mask"]), P(a["stats"]),
+                                      P(a["dlogp"]), P(a["ws"]), a["ws_bytes"], None)
+    assert st == status, binding.lib().pg_last_error()
+
+
+def test_workspace_sizes():
+    L = binding.lib()
+    for f in (L.pg_linear_fwd_workspace_size, L.pg_linear_bwd_workspace_size):
+        assert f(-1, 0, 0, 0, 1, 1, 64) == 0
+        assert 0 < f(1, 8, 4096, 5120, 32, 8, 128) < f(8, 128, 73275, 266240, 64, 8, 128)
+        # a state for each item: at least one a segment
+        assert f(1, 8, 4096, 5120, 32, 8, 128) >= 9 * 8 * 128 * 128 * 4
+    assert L.pg_token_logprobs_workspace_size(-1, 0, 0, 0) == 0 and L.pg_policy_loss_workspace_size(1, -1, 0) == 0
+    assert binding.token_logprobs_workspace_bytes(3, 9, 100, 1000) > 0
+    assert binding.policy_loss_workspace_bytes(3, 9, 100) < binding.policy_loss_workspace_bytes(3, 900, 100000)
+
+
+def _t(*s, dtype=torch.float32):
+    return torch.zeros(*s, dtype=dtype)
+
+
+def _i(*x):
+    return torch.tensor(x, dtype=torch.int32)
+
+
+def _lin_args():
+    return [_t(8, 4, 64), _t(8, 2, 64), _t(8, 2, 64), _t(6, 4, 64), _t(6, 2, 64), _t(6, 2, 64)], (_i(0, 8), _i(0, 2, 6), _i(2))
+
+
+def test_binding_refuses_host_and_misshapen_tensors():
+    x, grp = _lin_args()
+    with pytest.raises(ValueError, match="GPU device memory"):
+        binding.linear_fwd(*x, _t(2), *grp, 0.1)
+    with pytest.raises(ValueError, match="GPU device memory"):
+        binding.linear_step(_t(3, 4, 64), _t(3, 2, 64), _t(3, 2, 64), _t(3, 2, 64, 64), _t(2), 0.1)
+    with pytest.raises(ValueError, match="v_suf has shape"):
+        binding.linear_fwd(*x[:5], _t(6, 3, 64), _t(2), *grp, 0.1)
+    with pytest.raises(ValueError, match="contiguous"):
+        binding.linear_bwd(*x, _t(8, 64, 4).transpose(1, 2), _t(6, 4, 64), _t(2), *grp, 0.1)
+    with pytest.raises(TypeError, match="dtype"):
+        binding.linear_step(_t(3, 4, 64), _t(3, 2, 64, dtype=torch.bfloat16), _t(3, 2, 64), _t(3, 2, 64, 64), _t(2), 0.1)
+    logits, tok = _t(6, 10), torch.zeros(6, dtype=torch.int64)
+    with pytest.raises(ValueError, match="rows"):
+        binding.token_logprobs(_t(1, 10), _t(10, 6).t(), tok, *grp, 8)
+    with pytest.raises(TypeError, match="tokens"):
+        binding.token_logprobs(_t(1, 10), logits, tok.to(torch.int16), *grp, 8)
+    with pytest.raises(ValueError, match="logits_last has shape"):
+        binding.token_logprobs(_t(2, 10), logits, tok, *grp, 8)
+    with pytest.raises(ValueError, match="GPU device memory"):
+        binding.token_logprobs(_t(1, 10), logits, tok, *grp, 8)
+    with pytest.raises(ValueError, match="average"):
+        binding.policy_loss(_t(6), _t(2), *grp[1:], average="mean")
+    with pytest.raises(ValueError, match="advantages has shape"):
+        binding.policy_loss(_t(6), _t(3), *grp[1:])
