@@ -43,9 +43,12 @@ struct LinArgs {
   float* slots;           // [max_items + n_groups, h_kv, D, D]
   const int* seg_off;     // first item of each prefix, then of each member
   const LinItem* items;
+  const int* n_items;     // 0 when the grouping arrays are inconsistent
   const PlanHeader* hdr;
   const GroupInfoEx* ginfo;
   int ng, ns, h_q, h_kv, max_items;
+  int l_pre, l_suf;   // rows of a prefix's and of a member's items
+  int members_first;  // backward: the members' gradients are done before the prefixes' walk starts
   float scale;
 };
 
@@ -56,46 +59,51 @@ __device__ __forceinline__ float log2_decay(const float* log_decay, int h) {
 }
 
 // ---------------------------------------------------------------- items
-// One block: item offsets of all segments (prefixes, then members), then the items themselves.
-__global__ void __launch_bounds__(kPlanThreads) lin_items_kernel(const int* __restrict__ cu_p,
-                                                                 const int* __restrict__ cu_s, int ng, int ns, int L,
-                                                                 int max_items, int reverse, PlanHeader* hdr,
-                                                                 const GroupInfoEx* __restrict__ ginfo, int* seg_off,
-                                                                 LinItem* items) {
-  __shared__ int tmp[kPlanThreads];
-  __shared__ int carry;
+// One walk's items: where they go and how many rows they hold.
+struct LinList {
+  int* seg_off;     // [n_groups + n_suffixes + 1]
+  LinItem* items;   // [max_items]
+  int* n_items;
+  int l_pre, l_suf, max_items, reverse;
+};
+
+// One block: item offsets of all segments (prefixes, then members), then the items themselves. `off`: seg_off, or a
+// copy of it in LDS (then both are written).
+__device__ __forceinline__ void lin_items(const LinList& L, const int* cu_p, const int* cu_s, const GroupInfoEx* ginfo,
+                                          int ng, int ns, int* off, int* tmp, int& carry) {
   const int t = threadIdx.x, segs = ng + ns;
-  if (hdr->error) {
-    if (t == 0) hdr->n_qtiles = 0;
-    return;
-  }
+  __syncthreads();
   if (t == 0) carry = 0;
   __syncthreads();
   for (int base = 0; base < segs; base += kPlanThreads) {
     const int s = base + t;
     int n = 0;
-    if (s < segs) n = ceil_div(s < ng ? cu_p[s + 1] - cu_p[s] : cu_s[s - ng + 1] - cu_s[s - ng], L);
+    if (s < segs) n = s < ng ? ceil_div(cu_p[s + 1] - cu_p[s], L.l_pre) : ceil_div(cu_s[s - ng + 1] - cu_s[s - ng], L.l_suf);
     const int inc = block_inclusive_scan<kPlanThreads>(n, tmp);
-    if (s < segs) seg_off[s] = carry + inc - n;
+    if (s < segs) {
+      off[s] = carry + inc - n;
+      if (off != L.seg_off) L.seg_off[s] = off[s];
+    }
     __syncthreads();
     if (t == kPlanThreads - 1) carry += inc;
     __syncthreads();
   }
-  const int total = min(carry, max_items);
+  const int total = min(carry, L.max_items);
   if (t == 0) {
-    seg_off[segs] = total;
-    hdr->n_qtiles = total;
+    off[segs] = L.seg_off[segs] = total;
+    *L.n_items = total;
   }
   __syncthreads();
   for (int i = t; i < total; i += kPlanThreads) {
-    const int s = upper_index(seg_off, 0, segs, i), c = i - seg_off[s];
+    const int s = upper_index(off, 0, segs, i), c = i - off[s];
     LinItem it;
     it.part = s >= ng;
+    const int rows = it.part ? L.l_suf : L.l_pre;
     it.seg = it.part ? s - ng : s;
     const int lo = it.part ? cu_s[it.seg] : cu_p[s], hi = it.part ? cu_s[it.seg + 1] : cu_p[s + 1];
-    it.nrows = min(L, hi - lo - c * L);
-    it.row0 = reverse ? hi - c * L - it.nrows : lo + c * L;
-    it.last = c == ceil_div(hi - lo, L) - 1;
+    it.nrows = min(rows, hi - lo - c * rows);
+    it.row0 = L.reverse ? hi - c * rows - it.nrows : lo + c * rows;
+    it.last = c == ceil_div(hi - lo, rows) - 1;
     it.group = s;
     if (it.part) {
       int a = 0, b = ng;  // the group of the member: the last one whose members start at or before it
@@ -107,24 +115,61 @@ __global__ void __launch_bounds__(kPlanThreads) lin_items_kernel(const int* __re
     }
     if (c > 0) it.prev = i - 1;
     else if (!it.part) it.prev = kInitState;
-    else if (reverse) it.prev = kNoState;
-    else it.prev = cu_p[it.group + 1] > cu_p[it.group] ? seg_off[it.group + 1] - 1 : kInitState;
+    else if (L.reverse) it.prev = kNoState;
+    else it.prev = cu_p[it.group + 1] > cu_p[it.group] ? off[it.group + 1] - 1 : kInitState;
     it.pad = 0;
-    items[i] = it;
+    L.items[i] = it;
   }
 }
 
+// The items alone, behind plan_groups_kernel: for grouping arrays of any size.
+__global__ void __launch_bounds__(kPlanThreads) lin_items_kernel(const int* __restrict__ cu_p,
+                                                                 const int* __restrict__ cu_s, int ng, int ns,
+                                                                 const LinList L, const PlanHeader* hdr,
+                                                                 const GroupInfoEx* __restrict__ ginfo) {
+  __shared__ int tmp[kPlanThreads];
+  __shared__ int carry;
+  if (hdr->error) {
+    if (threadIdx.x == 0) *L.n_items = 0;
+    return;
+  }
+  lin_items(L, cu_p, cu_s, ginfo, ng, ns, L.seg_off, tmp, carry);
+}
+
+// Groups and the items of one walk or two in one launch, for grouping arrays that fit LDS (the usual case): three
+// launches of dependent one-block kernels cost 5 us each.
+__global__ void __launch_bounds__(kPlanThreads) lin_plan_kernel(const int* __restrict__ cu_p,
+                                                                const int* __restrict__ cu_s,
+                                                                const int* __restrict__ gsz, int ng, int ns, int tp,
+                                                                int ts, PlanHeader* hdr, GroupInfoEx* ginfo, int* qoff,
+                                                                int* kvoff, const LinList a, const LinList b,
+                                                                int lists) {
+  __shared__ PlanLds lds;
+  __shared__ int off[kLdsGroups + kLdsMembers + 1];
+  __shared__ int carry;
+  const bool ok = plan_groups_lds(cu_p, cu_s, gsz, ng, ns, tp, ts, kFwdBM, kKvBN, 1, 0, 0x7fffffffL, 0x7fffffffL, hdr,
+                                  ginfo, qoff, kvoff, lds);
+  __syncthreads();
+  if (!ok) {
+    if (threadIdx.x == 0) {
+      *a.n_items = 0;
+      if (lists > 1) *b.n_items = 0;
+    }
+    return;
+  }
+  lin_items(a, lds.cu_p, lds.cu_s, lds.gi, ng, ns, off, lds.part, carry);
+  if (lists > 1) lin_items(b, lds.cu_p, lds.cu_s, lds.gi, ng, ns, off, lds.part, carry);
+}
+
 // ---------------------------------------------------------------- pieces of the walks
-// Tile shapes: kC rows a chunk, kNW waves. 32-row chunks keep two workgroups of 128-wide bf16 heads on a CU.
-constexpr int kLinThreads = 256;
-template <typename T, int D>
-struct LinShape {
-  static constexpr int kNT = kLinThreads, kNW = kNT / 64;
-  static constexpr int kC = D == 128 ? 32 : 64;
-  static constexpr int kNB = D / 32;                // 32-wide blocks of a head
-  static constexpr int kNQ = kC / 32;               // 32-row tiles of a chunk
-  static constexpr int kAcc = kNB * kNB / kNW;      // 32 x 32 state tiles of a wave
-  static constexpr int kTileBytes = LdsTile<T, D>::bytes(kC);
+// Tile shapes of a walk: C rows a chunk, NW waves.
+template <typename T, int D, int C, int NW>
+struct LinTiles {
+  static constexpr int kC = C, kNW = NW, kNT = 64 * NW;
+  static constexpr int kNB = D / 32;            // 32-wide blocks of a head
+  static constexpr int kNQ = C / 32;            // 32-row tiles of a chunk
+  static constexpr int kAcc = kNB * kNB / NW;   // 32 x 32 state tiles of a wave
+  static constexpr int kTileBytes = LdsTile<T, D>::bytes(C);
   static constexpr int kStateBytes = LdsTile<T, D>::bytes(D);
 };
 
@@ -151,23 +196,48 @@ __device__ __forceinline__ Elt<float>::Frag row_perm(const char* tile, int row, 
   return f;
 }
 
-// acc[kb] (+)= sum over the chunk's rows of a_row^T (l^e(row) b_row), e = n-1-row (forward) or row (backward): a's
-// columns 32 (kb0 + kb).., b's columns 32 nb.. . Rows past the chunk's end are zero in both tiles.
-template <typename T, int D, bool REV, int SPLIT, int N>
-__device__ __forceinline__ void state_update(f32x16 (&acc)[N], const char* ta, const char* tb,
-                                             const FragOffsets<T, D>& fo, int kb0, int nb, int n, float g, int h) {
-  using S = LinShape<T, D>;
-  using E = Elt<T>;
-#pragma unroll
-  for (int t = 0; t < S::kC / 16; ++t) {
-    const typename E::Frag b = fo.tr(tb, t, nb);
-    float x[8];
+// The decays of a chunk's rows in a state update, l^e with e = n-1-row (forward) or row (backward), as products of a
+// power for the 16-row step and one for the lane's rows in it, both of exponents >= 0.
+template <bool REV>
+struct RowDecay {
+  float in_step[8];  // of row 4h + (s & 3) + 8 (s >> 2) of a 16-row step
+  float g;
+  int h;
+  __device__ __forceinline__ void init(float g_, int h_) {
+    g = g_;
+    h = h_;
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
-      const int row = 16 * t + 4 * h + (s & 3) + 8 * (s >> 2);
-      const int e = REV ? row : max(n - 1 - row, 0);
-      x[s] = E::frag_elem(b, s) * fast_exp2(g * (float)e);
+      const int row = 4 * h + (s & 3) + 8 * (s >> 2);
+      in_step[s] = fast_exp2(g * (float)(REV ? row : 15 - row));
     }
+  }
+  __device__ __forceinline__ void step(int t, int n, float (&w)[8]) const {
+    if (REV || 16 * t + 16 <= n) {
+      const float f = fast_exp2(g * (float)(REV ? 16 * t : n - 16 - 16 * t));
+#pragma unroll
+      for (int s = 0; s < 8; ++s) w[s] = f * in_step[s];
+    } else {  // the step that the chunk ends in: its rows past the end are zero
+#pragma unroll
+      for (int s = 0; s < 8; ++s) w[s] = fast_exp2(g * (float)max(n - 1 - 16 * t - (4 * h + (s & 3) + 8 * (s >> 2)), 0));
+    }
+  }
+};
+
+// acc[kb] += sum over the chunk's n rows of a_row^T (l^e(row) b_row): a's columns 32 (kb0 + kb).., b's columns 32 nb.. .
+template <typename T, int D, int C, bool REV, int SPLIT, int N>
+__device__ __forceinline__ void state_update(f32x16 (&acc)[N], const char* ta, const char* tb,
+                                             const FragOffsets<T, D>& fo, const RowDecay<REV>& rd, int kb0, int nb,
+                                             int n) {
+  using E = Elt<T>;
+#pragma unroll
+  for (int t = 0; t < C / 16; ++t) {
+    if (t > 0 && 16 * t >= n) break;
+    float w[8], x[8];
+    rd.step(t, n, w);
+    const typename E::Frag b = fo.tr(tb, t, nb);
+#pragma unroll
+    for (int s = 0; s < 8; ++s) x[s] = E::frag_elem(b, s) * w[s];
     typename E::Frag part[SPLIT];
 #pragma unroll
     for (int p = 0; p < SPLIT; ++p) {
@@ -186,6 +256,38 @@ __device__ __forceinline__ void state_update(f32x16 (&acc)[N], const char* ta, c
   }
 }
 
+// The decays of a 32 x 32 score tile (transposed: register r holds row 8 (r / 4) + 4h + r % 4 of the tile's rows, the
+// lane its column), from registers filled once: on the diagonal l^(dist) where dist >= 0, else 0; off it l^(31 - a)
+// l^(1 + b) l^(32 (tiles - 1)), a and b the earlier and the later row's place in its tile. REV: the registers run
+// over the later rows.
+template <bool REV>
+struct TileDecay {
+  float diag[16], reg[16], lane_f;
+  float g;
+  __device__ __forceinline__ void init(float g_, int lane) {
+    g = g_;
+    const int l = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int row = 8 * (r / 4) + 4 * h + r % 4, dist = REV ? row - l : l - row;
+      diag[r] = dist >= 0 ? fast_exp2(g * (float)dist) : 0.f;
+      reg[r] = fast_exp2(g * (float)(REV ? 1 + row : 31 - row));
+    }
+    lane_f = fast_exp2(g * (float)(REV ? 31 - l : 1 + l));
+  }
+  // sc *= decays, `tiles` tiles off the diagonal
+  __device__ __forceinline__ void apply(f32x16& sc, int tiles) const {
+    if (tiles == 0) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] *= diag[r];
+    } else {
+      const float f = lane_f * fast_exp2(g * (float)(32 * (tiles - 1)));
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] *= f * reg[r];
+    }
+  }
+};
+
 // A wave's state tiles: rows (of k) 32 (kb0 + kb) + 8 (r / 4) + 4h + r % 4, column (of v) 32 nb + lane % 32.
 template <int N>
 __device__ __forceinline__ void state_scale(f32x16 (&acc)[N], float f) {
@@ -196,11 +298,18 @@ __device__ __forceinline__ void state_scale(f32x16 (&acc)[N], float f) {
 }
 template <int D, int N>
 __device__ __forceinline__ void state_load(f32x16 (&acc)[N], const float* src, int kb0, int nb, int lane) {
+  if (src) {
 #pragma unroll
-  for (int i = 0; i < N; ++i)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-      acc[i][r] = src ? src[(32 * (kb0 + i) + 8 * (r / 4) + 4 * (lane >> 5) + r % 4) * D + 32 * nb + (lane & 31)] : 0.f;
+      for (int r = 0; r < 16; ++r)
+        acc[i][r] = src[(32 * (kb0 + i) + 8 * (r / 4) + 4 * (lane >> 5) + r % 4) * D + 32 * nb + (lane & 31)];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
+  }
 }
 template <int D, int N>
 __device__ __forceinline__ void state_store(const f32x16 (&acc)[N], float* dst, int kb0, int nb, int lane) {
@@ -221,6 +330,48 @@ __device__ __forceinline__ void state_to_lds(const f32x16 (&acc)[N], char* st, i
                      acc[i][4 * j], acc[i][4 * j + 1], acc[i][4 * j + 2], acc[i][4 * j + 3]);
 }
 
+// An item in scalar registers (it is the same for the whole workgroup; buffer descriptors are formed from it).
+__device__ __forceinline__ LinItem uniform_item(const LinItem* items, int i) {
+  LinItem it = items[i];
+  it.row0 = uniform(it.row0);
+  it.nrows = uniform(it.nrows);
+  it.part = uniform(it.part);
+  it.seg = uniform(it.seg);
+  it.prev = uniform(it.prev);
+  it.last = uniform(it.last);
+  it.group = uniform(it.group);
+  return it;
+}
+
+// Output tiles acc (transposed: register r of tile d holds column 32 (c0 + d) + 8 (r / 4) + 4h + r % 4 of the lane's
+// row) times `scale`, to row `row` of an LDS tile.
+template <typename T, int D, int N>
+__device__ __forceinline__ void rows_to_lds(const f32x16 (&acc)[N], char* tile, int row, int c0, int h, float scale) {
+#pragma unroll
+  for (int d = 0; d < N; ++d)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      Elt<T>::store4((T*)(tile + LdsTile<T, D>::elem_off(row, 32 * (c0 + d) + 8 * j + 4 * h)), scale * acc[d][4 * j],
+                     scale * acc[d][4 * j + 1], scale * acc[d][4 * j + 2], scale * acc[d][4 * j + 3]);
+}
+
+// The first `valid` rows of an LDS tile to memory, by the mapping of the loader that brings in such tiles: 16 bytes a
+// lane, whole rows by consecutive lanes (stores straight from the accumulators are 16-byte pieces of 32 rows each, and
+// cost the cache as much as full lines: 1270 -> 700 us without them where the outputs of 78k rows x 40 heads took 1270).
+// Rows past the range are dropped, without a branch: a wait for a later load would otherwise wait for the stores too.
+template <typename T, int ROWS, int D, int NT>
+__device__ __forceinline__ void tile_to_memory(const TileLoader<T, ROWS, D, NT>& m, const char* tile, T* base,
+                                               int gstride, int valid) {
+  typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+  const int bytes = range_bytes(valid, ROWS, gstride * (int)sizeof(T));
+  __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, bytes, 0x00020000);
+#pragma unroll
+  for (int i = 0; i < m.kPer; ++i) {
+    const u32x4 u = *(const u32x4*)(tile + m.loff + i * m.kRowStep * LdsTile<T, D>::kPitch);
+    __builtin_amdgcn_raw_buffer_store_b128(u, rs, m.goff + i * m.gstep, 0, 0);
+  }
+}
+
 // state before an item, NULL for zero
 template <int D>
 __device__ __forceinline__ const float* state_before(const LinArgs& a, const LinItem& it, int kv, bool reverse) {
@@ -234,75 +385,113 @@ __device__ __forceinline__ const float* state_before(const LinArgs& a, const Lin
 // ---------------------------------------------------------------- state kernel
 // An item's own share of the state after it. Forward: sum l^.. k v^T of one kv head; backward: sum l^.. q do^T over
 // the query heads that share it. Items whose state nobody reads are skipped: a member's last (forward), a prefix's
-// last (backward).
+// last (backward). The next tiles are loaded to registers while the present ones are used.
+template <typename T, int D>
+using LinStateTiles = LinTiles<T, D, D == 128 && sizeof(T) == 4 ? 32 : 64, 4>;
+constexpr int kLinStateThreads = 256;
 template <typename T, int D, bool REV, int SPLIT>
-__global__ void __launch_bounds__(kLinThreads, 2) lin_state_kernel(const LinArgs a) {
-  using S = LinShape<T, D>;
-  __shared__ __align__(16) char lds[2 * S::kTileBytes];
+__global__ void __launch_bounds__(kLinStateThreads, 2) lin_state_kernel(const LinArgs a) {
+  using S = LinStateTiles<T, D>;
+  static_assert(S::kNT == kLinStateThreads, "threads");
+  __shared__ __align__(16) char lds[2][2 * S::kTileBytes];
   const BlockSlot slot = xcd_slot(blockIdx.x, a.h_kv, 1);
-  if (slot.unit >= a.hdr->n_qtiles) return;  // 0 when the grouping arrays are inconsistent
-  const LinItem it = a.items[slot.unit];
-  if (it.last && it.part == (REV ? 0 : 1)) return;
+  if (slot.unit >= a.max_items) return;
+  const LinItem it = uniform_item(a.items, slot.unit);  // loaded beside the number of items, not behind it
+  if (slot.unit >= *a.n_items) return;
+  if (it.last && (it.part == (REV ? 0 : 1) || (REV && a.members_first))) return;
   const int kv = slot.head, ratio = a.h_q / a.h_kv;
   const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int nb = wave % S::kNB, kb0 = (wave / S::kNB) * S::kAcc;
   const float g = log2_decay(a.log_decay, kv);
-  const int heads = REV ? a.h_q : a.h_kv;
+  const int heads = REV ? a.h_q : a.h_kv, reps = REV ? ratio : 1;
   const T* pa = (const T*)(REV ? a.q[it.part] : a.k[it.part]);
   const T* pb = (const T*)(REV ? a.d_o[it.part] : a.v[it.part]);
   const int gs = heads * D;
-  Stager<T, S::kC, D, S::kNT> ld;
-  ld.init(gs, wave, lane);
-  Stager<T, S::kC, D, S::kNT> ld2;
-  ld2.init(gs, wave, lane);
+  TileLoader<T, S::kC, D, S::kNT> la, lb;
+  la.init(gs, wave, lane);
+  lb.init(gs, wave, lane);
   FragOffsets<T, D> fo;
   fo.init(lane);
+  RowDecay<REV> rd;
+  rd.init(g, lane >> 5);
   f32x16 acc[S::kAcc];
   state_load<D>(acc, nullptr, kb0, nb, lane);
-  char *ta = lds, *tb = lds + S::kTileBytes;
-  const int reps = REV ? ratio : 1;
-  for (int done = 0; done < it.nrows; done += S::kC) {
-    const int n = min(S::kC, it.nrows - done);
+  // step i: chunk i / reps, head i % reps
+  const int steps = ceil_div(it.nrows, S::kC) * reps;
+  auto load = [&](int i) {
+    const int done = i / reps * S::kC, n = min(S::kC, it.nrows - done);
     const int row = it.row0 + (REV ? it.nrows - done - n : done);
-    state_scale(acc, fast_exp2(g * (float)n));
-    for (int r = 0; r < reps; ++r) {
-      const size_t off = ((size_t)row * heads + (REV ? kv * ratio + r : kv)) * D;
-      ld.load(ta, pa + off, gs, n);
-      ld2.load(tb, pb + off, gs, n);
-      ld.store(ta);
-      ld2.store(tb);
-      ld.wait();
-      __syncthreads();
-      state_update<T, D, REV, SPLIT>(acc, ta, tb, fo, kb0, nb, n, g, lane >> 5);
-      __syncthreads();
-    }
+    const size_t off = ((size_t)row * heads + (REV ? kv * ratio + i % reps : kv)) * D;
+    la.load(nullptr, pa + off, gs, n);
+    lb.load(nullptr, pb + off, gs, n);
+  };
+  load(0);
+  for (int i = 0; i < steps; ++i) {
+    char *ta = lds[i & 1], *tb = ta + S::kTileBytes;
+    la.store(ta);
+    lb.store(tb);
+    __syncthreads();
+    if (i + 1 < steps) load(i + 1);
+    const int n = min(S::kC, it.nrows - i / reps * S::kC);
+    if (i % reps == 0) state_scale(acc, fast_exp2(g * (float)n));
+    state_update<T, D, S::kC, REV, SPLIT>(acc, ta, tb, fo, rd, kb0, nb, n);
   }
   state_store<D>(acc, a.slots + ((size_t)slot.unit * a.h_kv + kv) * (size_t)(D * D), kb0, nb, lane);
 }
 
 // ---------------------------------------------------------------- scans
-// In place over a segment's items: slot := l^rows (state before) + own share. One thread for four entries of a
-// state; grid (D * D / 1024, h_kv, segments). Prefixes (part 0) and members (part 1) are separate launches, members
-// first in a backward walk.
+// In place over a segment's items: slot := l^rows (state before) + own share. Prefixes (PART 0) and members (PART 1)
+// are separate launches, members first in a backward walk; grid (D * D / (256 V::kN), h_kv, segments). Chains of
+// dependent sums, all latency, so a thread has kBatch loads in flight. A prefix has many items and there are few
+// prefixes: one entry a thread, 32 loads; members have few items or none to do: four entries a thread, 8 loads, fewer
+// workgroups (P 16384 in 32 items, 16 members summed: 53 -> 16 us; 64 members with nothing to do 17 -> 6 us).
 constexpr int kScanThreads = 256;
-template <int D, bool REV>
-__global__ void __launch_bounds__(kScanThreads) lin_scan_kernel(const LinArgs a, int part) {
+template <int PART>
+struct ScanVec {
+  using type = float;
+  static constexpr int kN = 1, kBatch = 32;
+};
+template <>
+struct ScanVec<1> {
+  using type = f32x4;
+  static constexpr int kN = 4, kBatch = 8;
+};
+
+template <int D, bool REV, int PART>
+__global__ void __launch_bounds__(kScanThreads) lin_scan_kernel(const LinArgs a) {
+  using S = ScanVec<PART>;
+  using V = typename S::type;
+  constexpr int kBatch = S::kBatch;
   if (a.hdr->error) return;
   const int kv = blockIdx.y;
-  const size_t e = 4 * ((size_t)blockIdx.x * kScanThreads + threadIdx.x), per = (size_t)D * D;
+  const size_t e = S::kN * ((size_t)blockIdx.x * kScanThreads + threadIdx.x), per = (size_t)D * D;
   const float g = log2_decay(a.log_decay, kv);
-  auto at = [&](int slot) { return a.slots + ((size_t)slot * a.h_kv + kv) * per + e; };
-  for (int seg = blockIdx.z; seg < (part ? a.ns : a.ng); seg += gridDim.z) {
-    const int s = part ? a.ng + seg : seg;
+  auto at = [&](int slot) { return (V*)(a.slots + ((size_t)slot * a.h_kv + kv) * per + e); };
+  auto user = [&](const float* p, int seg) { return (V*)(p + ((size_t)seg * a.h_kv + kv) * per + e); };
+  const float full = fast_exp2(g * (float)(PART ? a.l_suf : a.l_pre));  // the rows of all items but a segment's last
+  for (int seg = blockIdx.z; seg < (PART ? a.ns : a.ng); seg += gridDim.z) {
+    const int s = PART ? a.ng + seg : seg;
     const int i0 = a.seg_off[s], i1 = a.seg_off[s + 1];
-    f32x4 st = {0.f, 0.f, 0.f, 0.f};
-    if (!part) {
+    V st = {};
+    if (!PART) {
       if (REV) {  // the members' states, in member order
-        for (int m = a.ginfo[seg].m0; m < a.ginfo[seg].m1; ++m)
-          if (a.seg_off[a.ng + m + 1] > a.seg_off[a.ng + m]) st += *(const f32x4*)at(a.seg_off[a.ng + m + 1] - 1);
-        *(f32x4*)at(a.max_items + seg) = st;
+        const int m0 = a.ginfo[seg].m0, m1 = a.ginfo[seg].m1;
+        for (int m = m0; m < m1; m += kBatch) {
+          V u[kBatch];
+#pragma unroll
+          for (int j = 0; j < kBatch; ++j) {
+            u[j] = V{};
+            if (m + j < m1) {
+              const int e0 = a.seg_off[a.ng + m + j], e1 = a.seg_off[a.ng + m + j + 1];
+              if (e1 > e0) u[j] = *at(e1 - 1);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < kBatch; ++j) st += u[j];
+        }
+        *at(a.max_items + seg) = st;
       } else if (a.state_in) {
-        st = *(const f32x4*)(a.state_in + ((size_t)seg * a.h_kv + kv) * per + e);
+        st = *user(a.state_in, seg);
       }
     } else if (!REV) {
       const bool handed = a.state_out[1] && i1 == i0;  // an empty member's state is its prefix's
@@ -313,109 +502,135 @@ __global__ void __launch_bounds__(kScanThreads) lin_scan_kernel(const LinArgs a,
         if (a.ginfo[mid].m0 <= seg) lo = mid; else hi = mid;
       }
       const int p0 = a.seg_off[lo], p1 = a.seg_off[lo + 1];
-      if (p1 > p0) st = *(const f32x4*)at(p1 - 1);
-      else if (a.state_in) st = *(const f32x4*)(a.state_in + ((size_t)lo * a.h_kv + kv) * per + e);
-      if (handed) *(f32x4*)(a.state_out[1] + ((size_t)seg * a.h_kv + kv) * per + e) = st;
+      if (p1 > p0) st = *at(p1 - 1);
+      else if (a.state_in) st = *user(a.state_in, lo);
+      if (handed) *user(a.state_out[1], seg) = st;
     }
-    // the last item's state has no reader in a prefix walked backwards and in a member walked forwards
-    const int end = (part != 0) == REV ? i1 : i1 - 1;
-    for (int i = i0; i < end; ++i) {
-      const f32x4 u = *(const f32x4*)at(i);
-      const float f = fast_exp2(g * (float)a.items[i].nrows);
-      st = st * f + u;
-      *(f32x4*)at(i) = st;
+    // the last item's state has no reader in a prefix walked backwards and in a member walked forwards; members_first:
+    // it is the gradient kernel that stores a member's
+    const int end = PART ? (REV && !a.members_first ? i1 : i1 - 1) : (REV ? i1 - 1 : i1);
+    for (int i = i0; i < end; i += kBatch) {
+      V u[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j)
+        if (i + j < end) u[j] = *at(i + j);
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j)
+        if (i + j < end) {
+          const float f = i + j < i1 - 1 ? full : fast_exp2(g * (float)a.items[i1 - 1].nrows);
+          st = st * f + u[j];
+          *at(i + j) = st;
+        }
     }
-    if (!part && !REV && a.state_out[0])
-      *(f32x4*)(a.state_out[0] + ((size_t)seg * a.h_kv + kv) * per + e) = st;
+    if (!PART && !REV && a.state_out[0]) *user(a.state_out[0], seg) = st;
   }
 }
 
 // ---------------------------------------------------------------- outputs (and dq, with the roles swapped)
-// One workgroup: one item, one query head. Wave w: query tile w % kNQ of each chunk, columns 32 kDT (w / kNQ).. .
+// One workgroup: one item and `hpw` of the query heads of one kv head, which share the keys, the values and the state
+// in LDS. Wave w: query rows 32 (w % kNQ).. of each chunk, columns 32 kDT (w / kNQ).. of the output. Queries come and
+// outputs go through LDS in whole rows; what the next head or chunk needs is loaded to registers meanwhile.
+template <typename T, int D>
+using LinOutTiles = LinTiles<T, D, D == 128 ? 32 : 64, 4>;
+constexpr int kLinThreads = 256;
+
 template <typename T, int D, int SPLIT>
-__global__ void __launch_bounds__(kLinThreads, 2) lin_out_kernel(const LinArgs a) {
-  using S = LinShape<T, D>;
+__global__ void __launch_bounds__(kLinThreads, sizeof(T) == 2 ? 2 : 1) lin_out_kernel(const LinArgs a, int hpw) {
+  using S = LinOutTiles<T, D>;
   using E = Elt<T>;
-  constexpr int kDT = S::kNB / (S::kNW / S::kNQ);
-  __shared__ __align__(16) char lds[3 * S::kTileBytes + S::kStateBytes];
-  const BlockSlot slot = xcd_slot(blockIdx.x, a.h_q, a.h_q / a.h_kv);
-  if (slot.unit >= a.hdr->n_qtiles) return;
-  const LinItem it = a.items[slot.unit];
-  const int hq = slot.head, ratio = a.h_q / a.h_kv, kv = hq / ratio;
+  static_assert(S::kNT == kLinThreads, "threads");
+  constexpr int kDT = S::kNB / (S::kNW / S::kNQ), kKK = D / 16;
+  __shared__ __align__(16) char lds[4 * S::kTileBytes + S::kStateBytes];
+  const int ratio = a.h_q / a.h_kv, parts = ratio / hpw;
+  const BlockSlot slot = xcd_slot(blockIdx.x, a.h_kv * parts, parts);
+  if (slot.unit >= a.max_items) return;
+  const LinItem it = uniform_item(a.items, slot.unit);  // loaded beside the number of items, not behind it
+  if (slot.unit >= *a.n_items) return;
+  const int kv = slot.head / parts, h0 = slot.head * hpw;
   const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, l = lane & 31;
   const int nb = wave % S::kNB, kb0 = (wave / S::kNB) * S::kAcc;
-  const int qi = wave % S::kNQ, dt0 = (wave / S::kNQ) * kDT;
+  const int qi = S::kNQ == 1 ? 0 : wave % S::kNQ, dt0 = (wave / S::kNQ) * kDT;
   const float g = log2_decay(a.log_decay, kv);
-  char *tq = lds, *tk = lds + S::kTileBytes, *tv = lds + 2 * S::kTileBytes, *ts = lds + 3 * S::kTileBytes;
-  Stager<T, S::kC, D, S::kNT> lq, lk, lv;
-  lq.init(a.h_q * D, wave, lane);
-  lk.init(a.h_kv * D, wave, lane);
-  lv.init(a.h_kv * D, wave, lane);
+  char *tk = lds, *tv = lds + S::kTileBytes, *tq = lds + 2 * S::kTileBytes, *to = lds + 3 * S::kTileBytes,
+       *ts = lds + 4 * S::kTileBytes;
+  const int gs = a.h_kv * D, gq = a.h_q * D;
+  TileLoader<T, S::kC, D, S::kNT> lk, lv, lq;
+  lk.init(gs, wave, lane);
+  lv.init(gs, wave, lane);
+  lq.init(gq, wave, lane);
   FragOffsets<T, D> fo;
   fo.init(lane);
+  RowDecay<false> rd;
+  rd.init(g, h);
+  TileDecay<false> td;
+  td.init(g, lane);
+  const float from_state = fast_exp2(g * (float)(32 * qi + l + 1));
   const T *q = (const T*)a.q[it.part], *k = (const T*)a.k[it.part], *v = (const T*)a.v[it.part];
   T* o = (T*)a.out[it.part];
   // the states are returned: the first query head of a kv head stores its member's
-  const bool keep = a.state_out[1] && it.part == 1 && it.last && hq == kv * ratio;
+  const bool keep = a.state_out[1] && it.part == 1 && it.last && slot.head % parts == 0;
 
   f32x16 acc[S::kAcc];
   state_load<D>(acc, state_before<D>(a, it, kv, false), kb0, nb, lane);
+  // past the item's end: an empty range, nothing is read
+  auto load_kv = [&](int done) {
+    const int n = min(S::kC, it.nrows - done);
+    const size_t at = ((size_t)(it.row0 + done) * a.h_kv + kv) * D;
+    lk.load(nullptr, k + at, gs, n);
+    lv.load(nullptr, v + at, gs, n);
+  };
+  auto load_q = [&](int done, int r) {
+    lq.load(nullptr, q + ((size_t)(it.row0 + done) * a.h_q + h0 + r) * D, gq, min(S::kC, it.nrows - done));
+  };
+  load_kv(0);
+  load_q(0, 0);
   for (int done = 0; done < it.nrows; done += S::kC) {
     const int n = min(S::kC, it.nrows - done);
-    const size_t row = it.row0 + done;
-    lq.load(tq, q + (row * a.h_q + hq) * D, a.h_q * D, n);
-    lk.load(tk, k + (row * a.h_kv + kv) * D, a.h_kv * D, n);
-    lv.load(tv, v + (row * a.h_kv + kv) * D, a.h_kv * D, n);
-    state_to_lds<T, D>(acc, ts, kb0, nb, lane);
-    lq.store(tq);
+    __syncthreads();  // the last chunk's keys, values and state have been read
     lk.store(tk);
     lv.store(tv);
-    lq.wait();
-    __syncthreads();
-    // the state's share, transposed (rows: columns of v; column: the query), scaled for the row's distance from it
-    f32x16 acc_o[kDT];
-#pragma unroll
-    for (int d = 0; d < kDT; ++d) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc_o[d][r] = 0.f;
-#pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk)
-        acc_o[d] = E::mma(fo.row(ts, 32 * (dt0 + d), kk), fo.row(tq, 32 * qi, kk), acc_o[d]);
-    }
-    state_scale(acc_o, fast_exp2(g * (float)(32 * qi + l + 1)));
-    // the chunk's own keys
-    for (int kt = 0; kt <= qi; ++kt) {
-      f32x16 sc;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] = 0.f;
-#pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) sc = E::mma(fo.row(tk, 32 * kt, kk), fo.row(tq, 32 * qi, kk), sc);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int dist = 32 * (qi - kt) + l - (8 * (r / 4) + 4 * h + r % 4);
-        sc[r] = dist >= 0 ? sc[r] * fast_exp2(g * (float)dist) : 0.f;
-      }
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const typename E::Frag p = E::acc_to_frag(sc, half);
-#pragma unroll
-        for (int d = 0; d < kDT; ++d) acc_o[d] = E::mma(fo.tr(tv, 2 * kt + half, dt0 + d), p, acc_o[d]);
-      }
-    }
-    if (32 * qi + l < n) {
-      T* dst = o + ((row + 32 * qi + l) * a.h_q + hq) * D;
+    state_to_lds<T, D>(acc, ts, kb0, nb, lane);
+    for (int r = 0; r < hpw; ++r) {
+      lq.store(tq);  // the last head's were read before the barrier in front of its outputs' way out
+      __syncthreads();
+      if (r == 0) load_kv(done + S::kC);
+      const bool last = r + 1 == hpw;
+      load_q(last ? done + S::kC : done, last ? 0 : r + 1);
+      // the state's share, transposed (rows: columns of v; column: the query), scaled for the row's distance from it
+      f32x16 acc_o[kDT];
 #pragma unroll
       for (int d = 0; d < kDT; ++d)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          E::store4(dst + 32 * (dt0 + d) + 8 * j + 4 * h, a.scale * acc_o[d][4 * j], a.scale * acc_o[d][4 * j + 1],
-                    a.scale * acc_o[d][4 * j + 2], a.scale * acc_o[d][4 * j + 3]);
+        for (int e = 0; e < 16; ++e) acc_o[d][e] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < kKK; ++kk)
+#pragma unroll
+        for (int d = 0; d < kDT; ++d)
+          acc_o[d] = E::mma(fo.row(ts, 32 * (dt0 + d), kk), fo.row(tq, 32 * qi, kk), acc_o[d]);
+      state_scale(acc_o, from_state);
+      // the chunk's own keys
+      for (int kt = 0; kt <= qi; ++kt) {
+        f32x16 sc;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < kKK; ++kk) sc = E::mma(fo.row(tk, 32 * kt, kk), fo.row(tq, 32 * qi, kk), sc);
+        td.apply(sc, S::kNQ == 1 ? 0 : qi - kt);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const typename E::Frag p = E::acc_to_frag(sc, half);
+#pragma unroll
+          for (int d = 0; d < kDT; ++d) acc_o[d] = E::mma(fo.tr(tv, 2 * kt + half, dt0 + d), p, acc_o[d]);
+        }
+      }
+      rows_to_lds<T, D>(acc_o, to, 32 * qi + l, dt0, h, a.scale);
+      __syncthreads();
+      tile_to_memory(lq, to, o + ((size_t)(it.row0 + done) * a.h_q + h0 + r) * D, gq, n);
     }
     if (done + n < it.nrows || keep) {
       state_scale(acc, fast_exp2(g * (float)n));
-      state_update<T, D, false, SPLIT>(acc, tk, tv, fo, kb0, nb, n, g, h);
+      state_update<T, D, S::kC, false, SPLIT>(acc, tk, tv, fo, rd, kb0, nb, n);
     }
-    __syncthreads();
   }
   if (keep) state_store<D>(acc, a.state_out[1] + ((size_t)it.seg * a.h_kv + kv) * (size_t)(D * D), kb0, nb, lane);
 }
@@ -423,70 +638,93 @@ __global__ void __launch_bounds__(kLinThreads, 2) lin_out_kernel(const LinArgs a
 // ---------------------------------------------------------------- dk, dv
 // One workgroup: one item, one kv head, walked backwards; the query heads that share it follow one another in each
 // chunk. Wave w: key rows 32 (w % kNQ).., and of the kNW / kNQ others the first half dv, the second dk, kWT tiles of
-// columns each.
+// columns each. Everything passes LDS in whole rows; what the next head or chunk needs is loaded to registers meanwhile.
+template <typename T, int D>
+using LinGradTiles = LinTiles<T, D, D == 128 ? 32 : 64, 4>;
+
 template <typename T, int D, int SPLIT>
-__global__ void __launch_bounds__(kLinThreads, 2) lin_grad_kernel(const LinArgs a) {
-  using S = LinShape<T, D>;
+__global__ void __launch_bounds__(kLinThreads, sizeof(T) == 2 ? 2 : 1) lin_grad_kernel(const LinArgs a, int only) {
+  using S = LinGradTiles<T, D>;
   using E = Elt<T>;
-  constexpr int kParts = S::kNW / S::kNQ, kWT = S::kNB / (kParts / 2);
+  static_assert(S::kNT == kLinThreads, "threads");
+  constexpr int kParts = S::kNW / S::kNQ, kWT = S::kNB / (kParts / 2), kKK = D / 16;
   __shared__ __align__(16) char lds[4 * S::kTileBytes + S::kStateBytes];
   const BlockSlot slot = xcd_slot(blockIdx.x, a.h_kv, 1);
-  if (slot.unit >= a.hdr->n_qtiles) return;
-  const LinItem it = a.items[slot.unit];
+  if (slot.unit >= a.max_items) return;
+  const LinItem it = uniform_item(a.items, slot.unit);  // loaded beside the number of items, not behind it
+  if (slot.unit >= *a.n_items) return;
+  if (only >= 0 && it.part != only) return;
   const int kv = slot.head, ratio = a.h_q / a.h_kv;
   const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, l = lane & 31;
   const int nb = wave % S::kNB, kb0 = (wave / S::kNB) * S::kAcc;
-  const int si = wave % S::kNQ, part = wave / S::kNQ;
+  const int si = S::kNQ == 1 ? 0 : wave % S::kNQ, part = wave / S::kNQ;
   const bool is_dk = part >= kParts / 2;
   const int ct0 = (part % (kParts / 2)) * kWT;
   const float g = log2_decay(a.log_decay, kv);
-  char *tk = lds, *tv = lds + S::kTileBytes, *tq = lds + 2 * S::kTileBytes, *td = lds + 3 * S::kTileBytes,
+  char *tk = lds, *tv = lds + S::kTileBytes, *tq = lds + 2 * S::kTileBytes, *tdo = lds + 3 * S::kTileBytes,
        *ts = lds + 4 * S::kTileBytes;
-  Stager<T, S::kC, D, S::kNT> lkv, lk2, lqd, lq2;
-  lkv.init(a.h_kv * D, wave, lane);
-  lk2.init(a.h_kv * D, wave, lane);
-  lqd.init(a.h_q * D, wave, lane);
-  lq2.init(a.h_q * D, wave, lane);
+  const int gs = a.h_kv * D, gq = a.h_q * D;
+  TileLoader<T, S::kC, D, S::kNT> lk, lv, lq, ld;
+  lk.init(gs, wave, lane);
+  lv.init(gs, wave, lane);
+  lq.init(gq, wave, lane);
+  ld.init(gq, wave, lane);
   FragOffsets<T, D> fo;
   fo.init(lane);
+  RowDecay<true> rd;
+  rd.init(g, h);
+  TileDecay<true> td;
+  td.init(g, lane);
   const T *q = (const T*)a.q[it.part], *k = (const T*)a.k[it.part], *v = (const T*)a.v[it.part],
           *d_o = (const T*)a.d_o[it.part];
-  T* out = (T*)(is_dk ? a.dk[it.part] : a.dv[it.part]);
-  const char* key = is_dk ? tv : tk;  // the key-side rows and the query-side rows of this wave's scores
-  const char* qry = is_dk ? td : tq;
-  const char* val = is_dk ? tq : td;  // what the scores weight
+  T *dk = (T*)a.dk[it.part], *dv = (T*)a.dv[it.part];
+  // members first: the prefix starts from what the members' last items store
+  const bool keep = a.members_first && it.part == 1 && it.last;
+  // this wave's key-side rows, query-side rows and what the scores weight
+  const char *key = is_dk ? tv : tk, *qry = is_dk ? tdo : tq, *val = is_dk ? tq : tdo;
 
   f32x16 acc[S::kAcc];
   state_load<D>(acc, state_before<D>(a, it, kv, true), kb0, nb, lane);
+  // the chunk that is `done` rows from the item's end: its number of rows (none past the item's start) and first row
+  auto rows = [&](int done) { return min(S::kC, it.nrows - done); };
+  auto first = [&](int done) { return (size_t)(it.row0 + max(it.nrows - done - S::kC, 0)); };
+  auto load_kv = [&](int done) {
+    const size_t at = (first(done) * a.h_kv + kv) * D;
+    lk.load(nullptr, k + at, gs, rows(done));
+    lv.load(nullptr, v + at, gs, rows(done));
+  };
+  auto load_q = [&](int done, int r) {
+    const size_t at = (first(done) * a.h_q + kv * ratio + r) * D;
+    lq.load(nullptr, q + at, gq, rows(done));
+    ld.load(nullptr, d_o + at, gq, rows(done));
+  };
+  load_kv(0);
+  load_q(0, 0);
   for (int done = 0; done < it.nrows; done += S::kC) {
-    const int n = min(S::kC, it.nrows - done);
-    const size_t row = it.row0 + (it.nrows - done - n);
-    lkv.load(tk, k + (row * a.h_kv + kv) * D, a.h_kv * D, n);
-    lk2.load(tv, v + (row * a.h_kv + kv) * D, a.h_kv * D, n);
+    const int n = rows(done);
+    lk.store(tk);
+    lv.store(tv);
     state_to_lds<T, D>(acc, ts, kb0, nb, lane);
-    lkv.store(tk);
-    lk2.store(tv);
     state_scale(acc, fast_exp2(g * (float)n));
     f32x16 acc_o[kWT];
     for (int r = 0; r < ratio; ++r) {
-      const size_t off = (row * a.h_q + kv * ratio + r) * D;
-      lqd.load(tq, q + off, a.h_q * D, n);
-      lq2.load(td, d_o + off, a.h_q * D, n);
-      lqd.store(tq);
-      lq2.store(td);
-      lqd.wait();
+      lq.store(tq);
+      ld.store(tdo);
       __syncthreads();
+      if (r == 0) load_kv(done + S::kC);
+      const bool last = r + 1 == ratio;
+      load_q(last ? done + S::kC : done, last ? 0 : r + 1);
       if (r == 0) {
 #pragma unroll
-        for (int c = 0; c < kWT; ++c) {
+        for (int w = 0; w < kWT; ++w) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) acc_o[c][e] = 0.f;
+          for (int e = 0; e < 16; ++e) acc_o[w][e] = 0.f;
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {
+          for (int kk = 0; kk < kKK; ++kk) {
             if (is_dk)  // the state's rows of k: a transposed read
-              acc_o[c] = E::mma(fo.tr(ts, kk, ct0 + c), row_perm<D>(tv, 32 * si + l, kk, h, T{}), acc_o[c]);
+              acc_o[w] = E::mma(fo.tr(ts, kk, ct0 + w), row_perm<D>(tv, 32 * si + l, kk, h, T{}), acc_o[w]);
             else
-              acc_o[c] = E::mma(fo.row(ts, 32 * (ct0 + c), kk), fo.row(tk, 32 * si, kk), acc_o[c]);
+              acc_o[w] = E::mma(fo.row(ts, 32 * (ct0 + w), kk), fo.row(tk, 32 * si, kk), acc_o[w]);
           }
         }
         state_scale(acc_o, fast_exp2(g * (float)max(n - 32 * si - l, 0)));
@@ -496,32 +734,27 @@ __global__ void __launch_bounds__(kLinThreads, 2) lin_grad_kernel(const LinArgs 
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[e] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) sc = E::mma(fo.row(qry, 32 * tt, kk), fo.row(key, 32 * si, kk), sc);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int dist = 32 * (tt - si) + (8 * (e / 4) + 4 * h + e % 4) - l;
-          sc[e] = dist >= 0 ? sc[e] * fast_exp2(g * (float)dist) : 0.f;
-        }
+        for (int kk = 0; kk < kKK; ++kk) sc = E::mma(fo.row(qry, 32 * tt, kk), fo.row(key, 32 * si, kk), sc);
+        td.apply(sc, S::kNQ == 1 ? 0 : tt - si);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const typename E::Frag p = E::acc_to_frag(sc, half);
 #pragma unroll
-          for (int c = 0; c < kWT; ++c) acc_o[c] = E::mma(fo.tr(val, 2 * tt + half, ct0 + c), p, acc_o[c]);
+          for (int w = 0; w < kWT; ++w) acc_o[w] = E::mma(fo.tr(val, 2 * tt + half, ct0 + w), p, acc_o[w]);
         }
       }
-      if (done + n < it.nrows) state_update<T, D, true, SPLIT>(acc, tq, td, fo, kb0, nb, n, g, h);
-      __syncthreads();
+      if (done + n < it.nrows || keep) state_update<T, D, S::kC, true, SPLIT>(acc, tq, tdo, fo, rd, kb0, nb, n);
+      __syncthreads();  // q, do (and after the last head k, v and the state) have been read
     }
-    if (32 * si + l < n) {
-      T* dst = out + ((row + 32 * si + l) * a.h_kv + kv) * D;
-#pragma unroll
-      for (int c = 0; c < kWT; ++c)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          E::store4(dst + 32 * (ct0 + c) + 8 * j + 4 * h, a.scale * acc_o[c][4 * j], a.scale * acc_o[c][4 * j + 1],
-                    a.scale * acc_o[c][4 * j + 2], a.scale * acc_o[c][4 * j + 3]);
-    }
+    // dv and dk go out through the tiles of q and do
+    rows_to_lds<T, D>(acc_o, is_dk ? tdo : tq, 32 * si + l, ct0, h, a.scale);
+    __syncthreads();
+    const size_t at = (first(done) * a.h_kv + kv) * D;
+    tile_to_memory(lk, tq, dv + at, gs, n);
+    tile_to_memory(lk, tdo, dk + at, gs, n);
+    __syncthreads();
   }
+  if (keep) state_store<D>(acc, a.slots + ((size_t)slot.unit * a.h_kv + kv) * (size_t)(D * D), kb0, nb, lane);
 }
 
 // ---------------------------------------------------------------- single tokens

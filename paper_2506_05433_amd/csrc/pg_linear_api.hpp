@@ -3,134 +3,184 @@
 
 namespace {
 
-// Rows an item holds. Long items save traffic (each costs a state written, scanned and read: 16 D^2 bytes a kv head),
-// short ones give more workgroups.
-int linear_item_rows(int tp, int ts, int heads) {
+// Rows an item of a prefix and of a member holds, of one walk with `heads` workgroups an item (query heads for
+// outputs, kv heads for gradients). Every item but a segment's last costs a state written, scanned and read (16 D^2
+// bytes a kv head) and its rows read once more; fewer items leave CUs idle.
+struct ItemRows {
+  int pre, suf;
+  int hpw;  // query heads a workgroup of the output kernel takes
+  bool members_first;
+};
+
+ItemRows linear_item_rows(int ns, int tp, int ts, int h_q, int h_kv, bool grad) {
+  ItemRows r{};
+  const int ratio = h_kv > 0 ? h_q / h_kv : 1;
   const long rows = (long)tp + ts;
-  int L = 2048;
-  while (L > 128 && rows * heads < 1024L * L) L /= 2;
-  return L;
+  r.hpw = 1;
+  if (!grad)
+    for (int d = 1; d <= ratio; ++d)
+      if (ratio % d == 0 && rows * h_kv * (ratio / d) >= 512L * 128) r.hpw = d;
+  const int heads = grad ? h_kv : h_q / r.hpw;
+  // prefixes: enough items to fill the CUs with state workgroups (one a kv head) and output workgroups
+  r.pre = 1024;
+  while (r.pre > 128 && (long)tp * h_kv < 256L * r.pre) r.pre /= 2;
+  // members: whole where there are enough of them (up to twice the mean length: a longer one is split), else as prefixes
+  const bool many = (long)ns * heads >= 512;
+  r.suf = 1024;
+  if (many)
+    while (r.suf < 65536 && (long)r.suf * ns < 2L * ts) r.suf *= 2;
+  else
+    while (r.suf > 128 && rows * heads < 512L * r.suf) r.suf /= 2;
+  r.members_first = many;
+  return r;
 }
 
 struct LinearLayout {
-  size_t hdr, ginfo, qoff, kvoff, seg_off, items, slots, total;
-  int L, max_items;
+  struct List {
+    ItemRows rows;
+    int max_items;
+    size_t seg_off, items;
+  };
+  size_t hdr, ginfo, qoff, kvoff, slots, total;
+  List out, grad;  // the forward walk (outputs, or dq); the backward one (dk, dv)
 };
 
-// Items of one walk: a segment of r rows has ceil(r / L).
-long linear_max_items(int ng, int ns, int tp, int ts, int L) {
-  return (long)tp / L + ng + (long)ts / L + ns;
-}
-
-LinearLayout linear_layout(int ng, int ns, int tp, int ts, int heads, int h_kv, int d) {
+LinearLayout linear_layout(int ng, int ns, int tp, int ts, int h_q, int h_kv, int d, bool bwd) {
   LinearLayout L{};
-  L.L = linear_item_rows(tp, ts, heads);
-  const long items = linear_max_items(ng, ns, tp, ts, L.L);
-  L.max_items = items > INT32_MAX ? -1 : (int)items;
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
   L.hdr = take(sizeof(pg::PlanHeader));
   L.ginfo = take(sizeof(pg::GroupInfoEx) * (size_t)(ng > 0 ? ng : 1));
   L.qoff = take(sizeof(int) * ((size_t)ng + 1));
   L.kvoff = take(sizeof(int) * ((size_t)ng + 1));
-  L.seg_off = take(sizeof(int) * ((size_t)ng + ns + 1));
-  L.items = take(sizeof(pg::LinItem) * (size_t)items);
-  L.slots = take(sizeof(float) * (size_t)(items + ng) * h_kv * d * d);
+  long most = 0;
+  auto list = [&](LinearLayout::List& l, bool grad) {
+    l.rows = linear_item_rows(ns, tp, ts, h_q, h_kv, grad);
+    // a segment of r rows has ceil(r / rows of an item) items
+    const long items = (long)tp / l.rows.pre + ng + (long)ts / l.rows.suf + ns;
+    l.max_items = items > INT32_MAX ? -1 : (int)items;
+    l.seg_off = take(sizeof(int) * ((size_t)ng + ns + 1));
+    l.items = take(sizeof(pg::LinItem) * (size_t)items);
+    most = std::max(most, items);
+  };
+  list(L.out, false);
+  if (bwd) list(L.grad, true);
+  L.slots = take(sizeof(float) * (size_t)(most + ng) * h_kv * d * d);  // the walks follow one another
   L.total = off;
   return L;
 }
 
-LinearLayout linear_fwd_layout(const Common& c) { return linear_layout(c.ng, c.ns, c.tp, c.ts, c.h_q, c.h_kv, c.d); }
-LinearLayout linear_bwd_layout(const Common& c) { return linear_layout(c.ng, c.ns, c.tp, c.ts, c.h_kv, c.h_kv, c.d); }
+template <int D, bool REV, int PART>
+void linear_scan(const Common& c, const pg::LinArgs& a, hipStream_t st) {
+  const int segs = PART ? c.ns : c.ng;
+  if (segs > 0)
+    hipLaunchKernelGGL((pg::lin_scan_kernel<D, REV, PART>),
+                       dim3(D * D / (pg::kScanThreads * pg::ScanVec<PART>::kN), c.h_kv, std::min(segs, 65535)),
+                       dim3(pg::kScanThreads), 0, st, a);
+}
 
-// One walk's plan, item shares and scans.
-template <typename T, int D, bool REV, int SPLIT>
-int linear_states(const Common& c, const LinearLayout& L, char* ws, const int32_t* cu_p, const int32_t* cu_s,
-                  const pg::LinArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(pg::lin_items_kernel, dim3(1), dim3(pg::kPlanThreads), 0, st, cu_p, cu_s, c.ng, c.ns, L.L,
-                     L.max_items, REV ? 1 : 0, (pg::PlanHeader*)(ws + L.hdr), a.ginfo, (int*)(ws + L.seg_off),
-                     (pg::LinItem*)(ws + L.items));
-  const long blocks = pg::xcd_grid_blocks(L.max_items, c.h_kv, 1);
-  hipLaunchKernelGGL((pg::lin_state_kernel<T, D, REV, SPLIT>), dim3((unsigned)blocks),
-                     dim3(pg::kLinThreads), 0, st, a);
-  for (int i = 0; i < 2; ++i) {
-    const int part = REV ? 1 - i : i, segs = part ? c.ns : c.ng;
-    if (segs > 0)
-      hipLaunchKernelGGL((pg::lin_scan_kernel<D, REV>), dim3(D * D / 1024, c.h_kv, std::min(segs, 65535)),
-                         dim3(pg::kScanThreads), 0, st, a, part);
+// Groups and items of the call's walks.
+int linear_plan(const Common& c, const LinearLayout& L, char* ws, const int32_t* cu_p, const int32_t* cu_s,
+                const int32_t* gsz, bool bwd, hipStream_t st) {
+  Timed tm(PG_K_PLAN, st);
+  auto* hdr = (pg::PlanHeader*)(ws + L.hdr);
+  auto* gi = (pg::GroupInfoEx*)(ws + L.ginfo);
+  auto list = [&](const LinearLayout::List& l, bool grad) {
+    return pg::LinList{(int*)(ws + l.seg_off), (pg::LinItem*)(ws + l.items), grad ? &hdr->n_kvtiles : &hdr->n_qtiles,
+                       l.rows.pre, l.rows.suf, l.max_items, grad ? 1 : 0};
+  };
+  const pg::LinList out = list(L.out, false), grad = bwd ? list(L.grad, true) : out;
+  if (pg::plan_fits_lds(c.ng, c.ns) && !plan_multi()) {
+    hipLaunchKernelGGL(pg::lin_plan_kernel, dim3(1), dim3(pg::kPlanThreads), 0, st, cu_p, cu_s, gsz, c.ng, c.ns, c.tp,
+                       c.ts, hdr, gi, (int*)(ws + L.qoff), (int*)(ws + L.kvoff), out, grad, bwd ? 2 : 1);
+    return finish_plan(hdr, st);
   }
+  int rc = launch_rope_plan(RopeLayout{L.hdr, L.ginfo, L.qoff, L.kvoff, 0}, ws, c.ng, c.ns, c.tp, c.ts, cu_p, cu_s, gsz,
+                            st);
+  if (rc) return rc;
+  for (int i = 0; i < (bwd ? 2 : 1); ++i)
+    hipLaunchKernelGGL(pg::lin_items_kernel, dim3(1), dim3(pg::kPlanThreads), 0, st, cu_p, cu_s, c.ng, c.ns,
+                       i ? grad : out, hdr, gi);
   return PG_OK;
 }
 
-template <typename T, int D, int SPLIT>
-void linear_out(const Common& c, const LinearLayout& L, const pg::LinArgs& a, hipStream_t st) {
-  const long blocks = pg::xcd_grid_blocks(L.max_items, c.h_q, c.h_q / c.h_kv);
-  hipLaunchKernelGGL((pg::lin_out_kernel<T, D, SPLIT>), dim3((unsigned)blocks), dim3(pg::kLinThreads), 0, st,
-                     a);
+// The items' own shares of one walk.
+template <typename T, int D, bool REV, int SPLIT>
+void linear_states(const Common& c, const pg::LinArgs& a, hipStream_t st) {
+  const long blocks = pg::xcd_grid_blocks(a.max_items, c.h_kv, 1);
+  hipLaunchKernelGGL((pg::lin_state_kernel<T, D, REV, SPLIT>), dim3((unsigned)blocks), dim3(pg::kLinStateThreads), 0,
+                     st, a);
 }
 
-void linear_common_args(pg::LinArgs& a, const Common& c, const LinearLayout& L, char* ws, const float* log_decay) {
+// The forward walk: shares, scans (prefixes, then the members that start from them), outputs.
+template <typename T, int D, int SPLIT>
+void linear_walk(const Common& c, int hpw, const pg::LinArgs& a, hipStream_t st) {
+  {
+    Timed tm(PG_K_LINEAR_STATE, st);
+    linear_states<T, D, false, SPLIT>(c, a, st);
+    linear_scan<D, false, 0>(c, a, st);
+    linear_scan<D, false, 1>(c, a, st);
+  }
+  Timed tm(PG_K_LINEAR_OUT, st);
+  const int parts = c.h_q / c.h_kv / hpw;
+  const long blocks = pg::xcd_grid_blocks(a.max_items, c.h_kv * parts, parts);
+  hipLaunchKernelGGL((pg::lin_out_kernel<T, D, SPLIT>), dim3((unsigned)blocks), dim3(pg::kLinThreads), 0, st, a, hpw);
+}
+
+void linear_common_args(pg::LinArgs& a, const Common& c, const LinearLayout& L, bool grad, char* ws,
+                        const float* log_decay) {
+  const LinearLayout::List& l = grad ? L.grad : L.out;
   a.log_decay = log_decay;
   a.slots = (float*)(ws + L.slots);
-  a.seg_off = (const int*)(ws + L.seg_off);
-  a.items = (const pg::LinItem*)(ws + L.items);
+  a.seg_off = (const int*)(ws + l.seg_off);
+  a.items = (const pg::LinItem*)(ws + l.items);
   a.hdr = (const pg::PlanHeader*)(ws + L.hdr);
+  a.n_items = grad ? &a.hdr->n_kvtiles : &a.hdr->n_qtiles;
   a.ginfo = (const pg::GroupInfoEx*)(ws + L.ginfo);
-  a.ng = c.ng; a.ns = c.ns; a.h_q = c.h_q; a.h_kv = c.h_kv; a.max_items = L.max_items;
+  a.ng = c.ng; a.ns = c.ns; a.h_q = c.h_q; a.h_kv = c.h_kv; a.max_items = l.max_items;
+  a.l_pre = l.rows.pre; a.l_suf = l.rows.suf;
+  a.members_first = l.rows.members_first;
   a.scale = c.scale;
 }
 
 template <typename T, int D>
-int linear_fwd_typed(const Common& c, const LinearLayout& L, char* ws, const int32_t* cu_p, const int32_t* cu_s,
-                     const pg::LinArgs& a, hipStream_t st) {
+void linear_fwd_typed(const Common& c, int hpw, const pg::LinArgs& a, hipStream_t st) {
   constexpr bool b16 = sizeof(T) == 2;
-  const bool states = a.state_out[0] || a.state_out[1];
-  {
-    Timed tm(PG_K_LINEAR_STATE, st);
-    if (states) linear_states<T, D, false, b16 ? 3 : 1>(c, L, ws, cu_p, cu_s, a, st);
-    else linear_states<T, D, false, b16 ? 2 : 1>(c, L, ws, cu_p, cu_s, a, st);
-  }
-  Timed tm(PG_K_LINEAR_OUT, st);
-  if (states) linear_out<T, D, b16 ? 3 : 1>(c, L, a, st);
-  else linear_out<T, D, b16 ? 2 : 1>(c, L, a, st);
-  return PG_OK;
+  if (a.state_out[0] || a.state_out[1]) linear_walk<T, D, b16 ? 3 : 1>(c, hpw, a, st);
+  else linear_walk<T, D, b16 ? 2 : 1>(c, hpw, a, st);
 }
 
 template <typename T, int D>
-int linear_bwd_typed(const Common& c, const LinearLayout& F, const LinearLayout& B, char* ws, const int32_t* cu_p,
-                     const int32_t* cu_s, const pg::LinArgs& dq, const pg::LinArgs& g, hipStream_t st) {
+void linear_bwd_typed(const Common& c, int hpw, const pg::LinArgs& dq, const pg::LinArgs& g, hipStream_t st) {
   constexpr int SPLIT = sizeof(T) == 2 ? 2 : 1;
+  linear_walk<T, D, SPLIT>(c, hpw, dq, st);
+  auto grad = [&](int part) {
+    Timed tm(PG_K_LINEAR_GRAD, st);
+    const long blocks = pg::xcd_grid_blocks(g.max_items, c.h_kv, 1);
+    hipLaunchKernelGGL((pg::lin_grad_kernel<T, D, SPLIT>), dim3((unsigned)blocks), dim3(pg::kLinThreads), 0, st, g, part);
+  };
   {
     Timed tm(PG_K_LINEAR_STATE, st);
-    linear_states<T, D, false, SPLIT>(c, F, ws, cu_p, cu_s, dq, st);
+    linear_states<T, D, true, SPLIT>(c, g, st);
+    linear_scan<D, true, 1>(c, g, st);
+    if (!g.members_first) linear_scan<D, true, 0>(c, g, st);
   }
-  {
-    Timed tm(PG_K_LINEAR_OUT, st);
-    linear_out<T, D, SPLIT>(c, F, dq, st);
-  }
+  if (!g.members_first) return grad(-1);
+  // the members' walks end with the states that the prefixes' start from: no pass over the responses for them alone
+  grad(1);
   {
     Timed tm(PG_K_LINEAR_STATE, st);
-    linear_states<T, D, true, SPLIT>(c, B, ws, cu_p, cu_s, g, st);
+    linear_scan<D, true, 0>(c, g, st);
   }
-  Timed tm(PG_K_LINEAR_GRAD, st);
-  const long blocks = pg::xcd_grid_blocks(B.max_items, c.h_kv, 1);
-  hipLaunchKernelGGL((pg::lin_grad_kernel<T, D, SPLIT>), dim3((unsigned)blocks), dim3(pg::kLinThreads), 0, st,
-                     g);
-  return PG_OK;
+  grad(0);
 }
 
-int linear_grid_check(const Common& c, const LinearLayout& L) {
+int linear_grid_check(const Common& c, const LinearLayout::List& l) {
   // workgroups of 256 threads, fewer than 2^32 threads a launch; item and slot numbers in 31 bits
-  if (L.max_items < 0 || (long)L.max_items + c.ng > INT32_MAX || ((long)L.max_items + 8) * c.h_q * 256 > 0xffffffffL ||
+  if (l.max_items < 0 || (long)l.max_items + c.ng > INT32_MAX || ((long)l.max_items + 8) * c.h_q * 256 > 0xffffffffL ||
       c.h_kv > 65535)
     return fail(PG_EUNSUPPORTED, "%d groups, %d members x %d heads exceed the launch grid", c.ng, c.ns, c.h_q);
   return PG_OK;
-}
-
-int plan_groups(const Common& c, char* ws, size_t hdr, size_t ginfo, size_t qoff, size_t kvoff, const int32_t* cu_p,
-                const int32_t* cu_s, const int32_t* gsz, hipStream_t st) {
-  Timed tp(PG_K_PLAN, st);
-  return launch_rope_plan(RopeLayout{hdr, ginfo, qoff, kvoff, 0}, ws, c.ng, c.ns, c.tp, c.ts, cu_p, cu_s, gsz, st);
 }
 
 bool misaligned(std::initializer_list<const void*> ps) {
@@ -147,15 +197,14 @@ size_t pg_linear_fwd_workspace_size(int n_groups, int n_suffixes, int total_pref
                                     int h_kv, int head_dim) {
   if (n_groups < 0 || n_suffixes < 0 || total_prefix < 0 || total_suffix < 0 || h_q < 0 || h_kv < 0 || head_dim < 0)
     return 0;
-  return linear_layout(n_groups, n_suffixes, total_prefix, total_suffix, h_q, h_kv, head_dim).total;
+  return linear_layout(n_groups, n_suffixes, total_prefix, total_suffix, h_q, h_kv, head_dim, false).total;
 }
 
 size_t pg_linear_bwd_workspace_size(int n_groups, int n_suffixes, int total_prefix, int total_suffix, int h_q,
                                     int h_kv, int head_dim) {
   if (n_groups < 0 || n_suffixes < 0 || total_prefix < 0 || total_suffix < 0 || h_q < 0 || h_kv < 0 || head_dim < 0)
     return 0;
-  return std::max(linear_layout(n_groups, n_suffixes, total_prefix, total_suffix, h_q, h_kv, head_dim).total,
-                  linear_layout(n_groups, n_suffixes, total_prefix, total_suffix, h_kv, h_kv, head_dim).total);
+  return linear_layout(n_groups, n_suffixes, total_prefix, total_suffix, h_q, h_kv, head_dim, true).total;
 }
 
 int pg_linear_fwd(int dtype, int n_groups, int n_suffixes, int total_prefix, int total_suffix,
@@ -173,29 +222,27 @@ int pg_linear_fwd(int dtype, int n_groups, int n_suffixes, int total_prefix, int
   if (total_suffix > 0 && (!q_suf || !k_suf || !v_suf || !o_suf)) return fail(PG_EINVAL, "a suffix tensor pointer is NULL");
   if (misaligned({q_pre, k_pre, v_pre, q_suf, k_suf, v_suf, state_in, o_pre, o_suf, state_pre, state_suf, workspace}))
     return fail(PG_EINVAL, "tensor pointers must be 16-byte aligned");
-  const LinearLayout L = linear_fwd_layout(c);
-  if ((rc = linear_grid_check(c, L))) return rc;
+  const LinearLayout L = linear_layout(c.ng, c.ns, c.tp, c.ts, c.h_q, c.h_kv, c.d, false);
+  if ((rc = linear_grid_check(c, L.out))) return rc;
   if (!workspace || workspace_bytes < L.total)
     return fail(PG_EWORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, L.total);
   if ((rc = device_ready())) return rc;
   if (c.ng == 0) return PG_OK;
   hipStream_t st = (hipStream_t)stream;
   char* ws = (char*)workspace;
-  if ((rc = plan_groups(c, ws, L.hdr, L.ginfo, L.qoff, L.kvoff, cu_prefix_lens, cu_suffix_lens, group_sizes, st)))
-    return rc;
+  if ((rc = linear_plan(c, L, ws, cu_prefix_lens, cu_suffix_lens, group_sizes, false, st))) return rc;
   pg::LinArgs a{};
-  linear_common_args(a, c, L, ws, log_decay);
+  linear_common_args(a, c, L, false, ws, log_decay);
   a.q[0] = q_pre; a.k[0] = k_pre; a.v[0] = v_pre; a.q[1] = q_suf; a.k[1] = k_suf; a.v[1] = v_suf;
   a.out[0] = o_pre; a.out[1] = o_suf;
   a.state_in = state_in;
   a.state_out[0] = state_pre; a.state_out[1] = state_suf;
-  if (dtype == PG_BF16)
-    rc = head_dim == 128 ? linear_fwd_typed<pg::bf16, 128>(c, L, ws, cu_prefix_lens, cu_suffix_lens, a, st)
-                         : linear_fwd_typed<pg::bf16, 64>(c, L, ws, cu_prefix_lens, cu_suffix_lens, a, st);
-  else
-    rc = head_dim == 128 ? linear_fwd_typed<float, 128>(c, L, ws, cu_prefix_lens, cu_suffix_lens, a, st)
-                         : linear_fwd_typed<float, 64>(c, L, ws, cu_prefix_lens, cu_suffix_lens, a, st);
-  if (rc) return rc;
+  const int hpw = L.out.rows.hpw;
+  if (dtype == PG_BF16) {
+    if (head_dim == 128) linear_fwd_typed<pg::bf16, 128>(c, hpw, a, st); else linear_fwd_typed<pg::bf16, 64>(c, hpw, a, st);
+  } else {
+    if (head_dim == 128) linear_fwd_typed<float, 128>(c, hpw, a, st); else linear_fwd_typed<float, 64>(c, hpw, a, st);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "linear attention forward launch");
   return PG_OK;
@@ -219,33 +266,32 @@ int pg_linear_bwd(int dtype, int n_groups, int n_suffixes, int total_prefix, int
   if (misaligned({q_pre, k_pre, v_pre, q_suf, k_suf, v_suf, do_pre, do_suf, dq_pre, dk_pre, dv_pre, dq_suf, dk_suf,
                   dv_suf, workspace}))
     return fail(PG_EINVAL, "tensor pointers must be 16-byte aligned");
-  const LinearLayout F = linear_fwd_layout(c), B = linear_bwd_layout(c);
-  if ((rc = linear_grid_check(c, F)) || (rc = linear_grid_check(c, B))) return rc;
-  const size_t need = std::max(F.total, B.total);
-  if (!workspace || workspace_bytes < need)
-    return fail(PG_EWORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, need);
+  const LinearLayout L = linear_layout(c.ng, c.ns, c.tp, c.ts, c.h_q, c.h_kv, c.d, true);
+  if ((rc = linear_grid_check(c, L.out)) || (rc = linear_grid_check(c, L.grad))) return rc;
+  if (!workspace || workspace_bytes < L.total)
+    return fail(PG_EWORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, L.total);
   if ((rc = device_ready())) return rc;
   if (c.ng == 0) return PG_OK;
   hipStream_t st = (hipStream_t)stream;
   char* ws = (char*)workspace;
-  if ((rc = plan_groups(c, ws, F.hdr, F.ginfo, F.qoff, F.kvoff, cu_prefix_lens, cu_suffix_lens, group_sizes, st)))
-    return rc;
+  if ((rc = linear_plan(c, L, ws, cu_prefix_lens, cu_suffix_lens, group_sizes, true, st))) return rc;
   // dq_t = c sum l^(t-s) (do_t . v_s) k_s: the forward walk with do, v, k in the places of q, k, v
   pg::LinArgs dq{}, g{};
-  linear_common_args(dq, c, F, ws, log_decay);
+  linear_common_args(dq, c, L, false, ws, log_decay);
   dq.q[0] = do_pre; dq.k[0] = v_pre; dq.v[0] = k_pre; dq.q[1] = do_suf; dq.k[1] = v_suf; dq.v[1] = k_suf;
   dq.out[0] = dq_pre; dq.out[1] = dq_suf;
-  linear_common_args(g, c, B, ws, log_decay);
+  linear_common_args(g, c, L, true, ws, log_decay);
   g.q[0] = q_pre; g.k[0] = k_pre; g.v[0] = v_pre; g.q[1] = q_suf; g.k[1] = k_suf; g.v[1] = v_suf;
   g.d_o[0] = do_pre; g.d_o[1] = do_suf;
   g.dk[0] = dk_pre; g.dk[1] = dk_suf; g.dv[0] = dv_pre; g.dv[1] = dv_suf;
-  if (dtype == PG_BF16)
-    rc = head_dim == 128 ? linear_bwd_typed<pg::bf16, 128>(c, F, B, ws, cu_prefix_lens, cu_suffix_lens, dq, g, st)
-                         : linear_bwd_typed<pg::bf16, 64>(c, F, B, ws, cu_prefix_lens, cu_suffix_lens, dq, g, st);
-  else
-    rc = head_dim == 128 ? linear_bwd_typed<float, 128>(c, F, B, ws, cu_prefix_lens, cu_suffix_lens, dq, g, st)
-                         : linear_bwd_typed<float, 64>(c, F, B, ws, cu_prefix_lens, cu_suffix_lens, dq, g, st);
-  if (rc) return rc;
+  const int hpw = L.out.rows.hpw;
+  if (dtype == PG_BF16) {
+    if (head_dim == 128) linear_bwd_typed<pg::bf16, 128>(c, hpw, dq, g, st);
+    else linear_bwd_typed<pg::bf16, 64>(c, hpw, dq, g, st);
+  } else {
+    if (head_dim == 128) linear_bwd_typed<float, 128>(c, hpw, dq, g, st);
+    else linear_bwd_typed<float, 64>(c, hpw, dq, g, st);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "linear attention backward launch");
   return PG_OK;
