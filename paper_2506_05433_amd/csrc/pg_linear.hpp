@@ -27,9 +27,9 @@
 namespace pg {
 
 // rows [row0, row0 + nrows) of a prefix (part 0) or of a member's response (part 1); seg: the group or member.
-// prev: slot of the state before it, kNoState, or kInitState (the group's initial state).
+// prev: slot of the state before it, kNoState, or kInitState (the group's initial state); self: its own slot.
 struct LinItem {
-  int row0, nrows, part, seg, prev, last, group, pad;
+  int row0, nrows, part, seg, prev, last, group, self;
 };
 constexpr int kNoState = -1, kInitState = -2;
 
@@ -44,6 +44,7 @@ struct LinArgs {
   const int* seg_off;     // first item of each prefix, then of each member
   const LinItem* items;
   const int* n_items;     // 0 when the grouping arrays are inconsistent
+  const int *cu_p, *cu_s;
   const PlanHeader* hdr;
   const GroupInfoEx* ginfo;
   int ng, ns, h_q, h_kv, max_items;
@@ -65,12 +66,21 @@ struct LinList {
   LinItem* items;   // [max_items]
   int* n_items;
   int l_pre, l_suf, max_items, reverse;
+  int round;  // workgroups' places: see item_place; 0: items in order
 };
+
+// Place in the launch of the item of rank r by length (0 the longest) among n. Items that are whole members differ in
+// length, and two workgroups share a CU: the `round` longest go first, one to a CU, the next `round` in the opposite
+// order, the shortest beside the longest, what is left longest first (64 members of 128..2048 rows: the output kernel
+// 584 -> 521 us, dk and dv 679 -> 585).
+__device__ __forceinline__ int item_place(int r, int n, int round) {
+  return r < round || r >= 2 * round ? r : min(2 * round, n) - 1 - (r - round);
+}
 
 // One block: item offsets of all segments (prefixes, then members), then the items themselves. `off`: seg_off, or a
 // copy of it in LDS (then both are written).
 __device__ __forceinline__ void lin_items(const LinList& L, const int* cu_p, const int* cu_s, const GroupInfoEx* ginfo,
-                                          int ng, int ns, int* off, int* tmp, int& carry) {
+                                          int ng, int ns, int* off, int* tmp, int& carry, int* work) {
   const int t = threadIdx.x, segs = ng + ns;
   __syncthreads();
   if (t == 0) carry = 0;
@@ -94,31 +104,41 @@ __device__ __forceinline__ void lin_items(const LinList& L, const int* cu_p, con
     *L.n_items = total;
   }
   __syncthreads();
-  for (int i = t; i < total; i += kPlanThreads) {
-    const int s = upper_index(off, 0, segs, i), c = i - off[s];
-    LinItem it;
-    it.part = s >= ng;
-    const int rows = it.part ? L.l_suf : L.l_pre;
-    it.seg = it.part ? s - ng : s;
-    const int lo = it.part ? cu_s[it.seg] : cu_p[s], hi = it.part ? cu_s[it.seg + 1] : cu_p[s + 1];
-    it.nrows = min(rows, hi - lo - c * rows);
-    it.row0 = L.reverse ? hi - c * rows - it.nrows : lo + c * rows;
-    it.last = c == ceil_div(hi - lo, rows) - 1;
-    it.group = s;
-    if (it.part) {
-      int a = 0, b = ng;  // the group of the member: the last one whose members start at or before it
-      while (b - a > 1) {
-        const int mid = (a + b) >> 1;
-        if (ginfo[mid].m0 <= it.seg) a = mid; else b = mid;
+  const bool ranked = work && L.round > 0 && total <= kPlanThreads;
+  for (int i = t; i < total || ranked; i += kPlanThreads) {
+    LinItem it = {};
+    if (i < total) {
+      const int s = upper_index(off, 0, segs, i), c = i - off[s];
+      it.part = s >= ng;
+      const int rows = it.part ? L.l_suf : L.l_pre;
+      it.seg = it.part ? s - ng : s;
+      const int lo = it.part ? cu_s[it.seg] : cu_p[s], hi = it.part ? cu_s[it.seg + 1] : cu_p[s + 1];
+      it.nrows = min(rows, hi - lo - c * rows);
+      it.row0 = L.reverse ? hi - c * rows - it.nrows : lo + c * rows;
+      it.last = c == ceil_div(hi - lo, rows) - 1;
+      it.group = s;
+      if (it.part) {
+        int a = 0, b = ng;  // the group of the member: the last one whose members start at or before it
+        while (b - a > 1) {
+          const int mid = (a + b) >> 1;
+          if (ginfo[mid].m0 <= it.seg) a = mid; else b = mid;
+        }
+        it.group = a;
       }
-      it.group = a;
+      if (c > 0) it.prev = i - 1;
+      else if (!it.part) it.prev = kInitState;
+      else if (L.reverse) it.prev = kNoState;
+      else it.prev = cu_p[it.group + 1] > cu_p[it.group] ? off[it.group + 1] - 1 : kInitState;
+      it.self = i;
     }
-    if (c > 0) it.prev = i - 1;
-    else if (!it.part) it.prev = kInitState;
-    else if (L.reverse) it.prev = kNoState;
-    else it.prev = cu_p[it.group + 1] > cu_p[it.group] ? off[it.group + 1] - 1 : kInitState;
-    it.pad = 0;
-    L.items[i] = it;
+    if (!ranked) {
+      L.items[i] = it;
+      continue;
+    }
+    work[t] = i < total ? it.nrows : -1;  // one item a thread
+    __syncthreads();
+    if (i < total) L.items[item_place(rank_among(work, 0, (total + 3) & ~3, 0, it.nrows, i), total, L.round)] = it;
+    break;
   }
 }
 
@@ -133,7 +153,7 @@ __global__ void __launch_bounds__(kPlanThreads) lin_items_kernel(const int* __re
     if (threadIdx.x == 0) *L.n_items = 0;
     return;
   }
-  lin_items(L, cu_p, cu_s, ginfo, ng, ns, L.seg_off, tmp, carry);
+  lin_items(L, cu_p, cu_s, ginfo, ng, ns, L.seg_off, tmp, carry, nullptr);
 }
 
 // Groups and the items of one walk or two in one launch, for grouping arrays that fit LDS (the usual case): three
@@ -157,8 +177,8 @@ __global__ void __launch_bounds__(kPlanThreads) lin_plan_kernel(const int* __res
     }
     return;
   }
-  lin_items(a, lds.cu_p, lds.cu_s, lds.gi, ng, ns, off, lds.part, carry);
-  if (lists > 1) lin_items(b, lds.cu_p, lds.cu_s, lds.gi, ng, ns, off, lds.part, carry);
+  lin_items(a, lds.cu_p, lds.cu_s, lds.gi, ng, ns, off, lds.part, carry, lds.work[0]);
+  if (lists > 1) lin_items(b, lds.cu_p, lds.cu_s, lds.gi, ng, ns, off, lds.part, carry, lds.work[1]);
 }
 
 // ---------------------------------------------------------------- pieces of the walks
@@ -340,6 +360,7 @@ __device__ __forceinline__ LinItem uniform_item(const LinItem* items, int i) {
   it.prev = uniform(it.prev);
   it.last = uniform(it.last);
   it.group = uniform(it.group);
+  it.self = uniform(it.self);
   return it;
 }
 
@@ -436,7 +457,7 @@ __global__ void __launch_bounds__(kLinStateThreads, 2) lin_state_kernel(const Li
     if (i % reps == 0) state_scale(acc, fast_exp2(g * (float)n));
     state_update<T, D, S::kC, REV, SPLIT>(acc, ta, tb, fo, rd, kb0, nb, n);
   }
-  state_store<D>(acc, a.slots + ((size_t)slot.unit * a.h_kv + kv) * (size_t)(D * D), kb0, nb, lane);
+  state_store<D>(acc, a.slots + ((size_t)it.self * a.h_kv + kv) * (size_t)(D * D), kb0, nb, lane);
 }
 
 // ---------------------------------------------------------------- scans
@@ -472,6 +493,9 @@ __global__ void __launch_bounds__(kScanThreads) lin_scan_kernel(const LinArgs a)
   for (int seg = blockIdx.z; seg < (PART ? a.ns : a.ng); seg += gridDim.z) {
     const int s = PART ? a.ng + seg : seg;
     const int i0 = a.seg_off[s], i1 = a.seg_off[s + 1];
+    // the last item holds what the others leave
+    const int len = PART ? a.cu_s[seg + 1] - a.cu_s[seg] : a.cu_p[seg + 1] - a.cu_p[seg];
+    const float tail = fast_exp2(g * (float)(len - max(i1 - i0 - 1, 0) * (PART ? a.l_suf : a.l_pre)));
     V st = {};
     if (!PART) {
       if (REV) {  // the members' states, in member order
@@ -517,7 +541,7 @@ __global__ void __launch_bounds__(kScanThreads) lin_scan_kernel(const LinArgs a)
 #pragma unroll
       for (int j = 0; j < kBatch; ++j)
         if (i + j < end) {
-          const float f = i + j < i1 - 1 ? full : fast_exp2(g * (float)a.items[i1 - 1].nrows);
+          const float f = i + j < i1 - 1 ? full : tail;
           st = st * f + u[j];
           *at(i + j) = st;
         }
@@ -754,7 +778,7 @@ __global__ void __launch_bounds__(kLinThreads, sizeof(T) == 2 ? 2 : 1) lin_grad_
     tile_to_memory(lk, tdo, dk + at, gs, n);
     __syncthreads();
   }
-  if (keep) state_store<D>(acc, a.slots + ((size_t)slot.unit * a.h_kv + kv) * (size_t)(D * D), kb0, nb, lane);
+  if (keep) state_store<D>(acc, a.slots + ((size_t)it.self * a.h_kv + kv) * (size_t)(D * D), kb0, nb, lane);
 }
 
 // ---------------------------------------------------------------- single tokens

@@ -10,6 +10,7 @@ struct ItemRows {
   int pre, suf;
   int hpw;  // query heads a workgroup of the output kernel takes
   bool members_first;
+  int round;  // items that fill the CUs once, where they are ordered by length (pg_linear.hpp, item_place)
 };
 
 ItemRows linear_item_rows(int ns, int tp, int ts, int h_q, int h_kv, bool grad) {
@@ -32,6 +33,7 @@ ItemRows linear_item_rows(int ns, int tp, int ts, int h_q, int h_kv, bool grad) 
   else
     while (r.suf > 128 && rows * heads < 512L * r.suf) r.suf /= 2;
   r.members_first = many;
+  r.round = many ? (int)ceil_div_l(256, heads) : 0;
   return r;
 }
 
@@ -87,7 +89,7 @@ int linear_plan(const Common& c, const LinearLayout& L, char* ws, const int32_t*
   auto* gi = (pg::GroupInfoEx*)(ws + L.ginfo);
   auto list = [&](const LinearLayout::List& l, bool grad) {
     return pg::LinList{(int*)(ws + l.seg_off), (pg::LinItem*)(ws + l.items), grad ? &hdr->n_kvtiles : &hdr->n_qtiles,
-                       l.rows.pre, l.rows.suf, l.max_items, grad ? 1 : 0};
+                       l.rows.pre, l.rows.suf, l.max_items, grad ? 1 : 0, l.rows.round};
   };
   const pg::LinList out = list(L.out, false), grad = bwd ? list(L.grad, true) : out;
   if (pg::plan_fits_lds(c.ng, c.ns) && !plan_multi()) {
@@ -128,9 +130,10 @@ void linear_walk(const Common& c, int hpw, const pg::LinArgs& a, hipStream_t st)
 }
 
 void linear_common_args(pg::LinArgs& a, const Common& c, const LinearLayout& L, bool grad, char* ws,
-                        const float* log_decay) {
+                        const float* log_decay, const int32_t* cu_p, const int32_t* cu_s) {
   const LinearLayout::List& l = grad ? L.grad : L.out;
   a.log_decay = log_decay;
+  a.cu_p = cu_p; a.cu_s = cu_s;
   a.slots = (float*)(ws + L.slots);
   a.seg_off = (const int*)(ws + l.seg_off);
   a.items = (const pg::LinItem*)(ws + l.items);
@@ -232,7 +235,7 @@ int pg_linear_fwd(int dtype, int n_groups, int n_suffixes, int total_prefix, int
   char* ws = (char*)workspace;
   if ((rc = linear_plan(c, L, ws, cu_prefix_lens, cu_suffix_lens, group_sizes, false, st))) return rc;
   pg::LinArgs a{};
-  linear_common_args(a, c, L, false, ws, log_decay);
+  linear_common_args(a, c, L, false, ws, log_decay, cu_prefix_lens, cu_suffix_lens);
   a.q[0] = q_pre; a.k[0] = k_pre; a.v[0] = v_pre; a.q[1] = q_suf; a.k[1] = k_suf; a.v[1] = v_suf;
   a.out[0] = o_pre; a.out[1] = o_suf;
   a.state_in = state_in;
@@ -277,10 +280,10 @@ int pg_linear_bwd(int dtype, int n_groups, int n_suffixes, int total_prefix, int
   if ((rc = linear_plan(c, L, ws, cu_prefix_lens, cu_suffix_lens, group_sizes, true, st))) return rc;
   // dq_t = c sum l^(t-s) (do_t . v_s) k_s: the forward walk with do, v, k in the places of q, k, v
   pg::LinArgs dq{}, g{};
-  linear_common_args(dq, c, L, false, ws, log_decay);
+  linear_common_args(dq, c, L, false, ws, log_decay, cu_prefix_lens, cu_suffix_lens);
   dq.q[0] = do_pre; dq.k[0] = v_pre; dq.v[0] = k_pre; dq.q[1] = do_suf; dq.k[1] = v_suf; dq.v[1] = k_suf;
   dq.out[0] = dq_pre; dq.out[1] = dq_suf;
-  linear_common_args(g, c, L, true, ws, log_decay);
+  linear_common_args(g, c, L, true, ws, log_decay, cu_prefix_lens, cu_suffix_lens);
   g.q[0] = q_pre; g.k[0] = k_pre; g.v[0] = v_pre; g.q[1] = q_suf; g.k[1] = k_suf; g.v[1] = v_suf;
   g.d_o[0] = do_pre; g.d_o[1] = do_suf;
   g.dk[0] = dk_pre; g.dk[1] = dk_suf; g.dv[0] = dv_pre; g.dv[1] = dv_suf;
