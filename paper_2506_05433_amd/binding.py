@@ -102,7 +102,7 @@ def _check(status: int):
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _dtype_code(torch, dt):
@@ -111,6 +111,18 @@ def _dtype_code(torch, dt):
     if dt == torch.float32:
         return PG_FP32
     raise TypeError(f"unsupported dtype {dt}")
+
+
+def _launch(dev, fn, *args):
+    """fn(*args, the current stream of ``dev``), with ``dev`` as the current device (a kernel is launched there)."""
+    import torch
+    if torch.cuda.current_device() == dev.index:
+        st = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    if st:
+        _check(st)
 
 
 def _stream(torch, device):
@@ -145,7 +157,7 @@ def _expect(device, dtype, **tensors):
         want = torch.float32 if dtype is None or name.startswith("lse") else dtype
         if not isinstance(t, torch.Tensor):
             raise TypeError(f"{name} must be a tensor")
-        if tuple(t.shape) != tuple(shape):
+        if t.shape != shape and tuple(t.shape) != tuple(shape):
             raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
         if t.dtype != want:
             raise TypeError(f"{name} has dtype {t.dtype}, expected {want}")
@@ -418,13 +430,11 @@ def linear_fwd(q_pre, k_pre, v_pre, q_suf, k_suf, v_suf, log_decay, cu_prefix, c
     _expect(dev, None, **f32)
     _grouping(dev, cu_prefix=(ng + 1, cu_prefix), cu_suffix=(ns + 1, cu_suffix), group_sizes=(ng, group_sizes))
     _workspace(workspace, dev)
-    with torch.cuda.device(dev):
-        st = lib().pg_linear_fwd(
-            _dtype_code(torch, dt), ng, ns, tp, ts, _ptr(cu_prefix), _ptr(cu_suffix), _ptr(group_sizes), hq, hkv, d,
-            float(scale), _ptr(log_decay), _ptr(q_pre), _ptr(k_pre), _ptr(v_pre), _ptr(q_suf), _ptr(k_suf), _ptr(v_suf),
-            _ptr(state_in), _ptr(out[0]), _ptr(out[1]), _ptr(out[2]) if states else None,
-            _ptr(out[3]) if states else None, _ptr(workspace), workspace.numel(), _stream(torch, dev))
-    _check(st)
+    _launch(
+        dev, lib().pg_linear_fwd, _dtype_code(torch, dt), ng, ns, tp, ts, _ptr(cu_prefix), _ptr(cu_suffix),
+        _ptr(group_sizes), hq, hkv, d, float(scale), _ptr(log_decay), _ptr(q_pre), _ptr(k_pre), _ptr(v_pre),
+        _ptr(q_suf), _ptr(k_suf), _ptr(v_suf), _ptr(state_in), _ptr(out[0]), _ptr(out[1]), _ptr(out[2]) if states
+        else None, _ptr(out[3]) if states else None, _ptr(workspace), workspace.numel())
     return tuple(out[:4] if states else out[:2])
 
 
@@ -446,13 +456,11 @@ def linear_bwd(q_pre, k_pre, v_pre, q_suf, k_suf, v_suf, do_pre, do_suf, log_dec
     _expect(dev, None, log_decay=((hkv,), log_decay))
     _grouping(dev, cu_prefix=(ng + 1, cu_prefix), cu_suffix=(ns + 1, cu_suffix), group_sizes=(ng, group_sizes))
     _workspace(workspace, dev)
-    with torch.cuda.device(dev):
-        st = lib().pg_linear_bwd(
-            _dtype_code(torch, dt), ng, ns, tp, ts, _ptr(cu_prefix), _ptr(cu_suffix), _ptr(group_sizes), hq, hkv, d,
-            float(scale), _ptr(log_decay), _ptr(q_pre), _ptr(k_pre), _ptr(v_pre), _ptr(q_suf), _ptr(k_suf), _ptr(v_suf),
-            _ptr(do_pre), _ptr(do_suf), *[_ptr(t) for t in out], _ptr(workspace), workspace.numel(),
-            _stream(torch, dev))
-    _check(st)
+    _launch(
+        dev, lib().pg_linear_bwd, _dtype_code(torch, dt), ng, ns, tp, ts, _ptr(cu_prefix), _ptr(cu_suffix),
+        _ptr(group_sizes), hq, hkv, d, float(scale), _ptr(log_decay), _ptr(q_pre), _ptr(k_pre), _ptr(v_pre),
+        _ptr(q_suf), _ptr(k_suf), _ptr(v_suf), _ptr(do_pre), _ptr(do_suf), *[_ptr(t) for t in out],
+        _ptr(workspace), workspace.numel())
     return tuple(out)
 
 
@@ -468,10 +476,9 @@ def linear_step(q, k, v, state, log_decay, scale, out=None):
         out = (torch.empty_like(q), state)
     _expect(dev, q.dtype, q=((n, hq, d), q), k=((n, hkv, d), k), v=((n, hkv, d), v), o=((n, hq, d), out[0]))
     _expect(dev, None, log_decay=((hkv,), log_decay), state=((n, hkv, d, d), state), state_out=((n, hkv, d, d), out[1]))
-    with torch.cuda.device(dev):
-        st = lib().pg_linear_step(_dtype_code(torch, q.dtype), n, hq, hkv, d, float(scale), _ptr(log_decay), _ptr(q),
-                                  _ptr(k), _ptr(v), _ptr(state), _ptr(out[0]), _ptr(out[1]), _stream(torch, dev))
-    _check(st)
+    _launch(
+        dev, lib().pg_linear_step, _dtype_code(torch, q.dtype), n, hq, hkv, d, float(scale), _ptr(log_decay),
+        _ptr(q), _ptr(k), _ptr(v), _ptr(state), _ptr(out[0]), _ptr(out[1]))
     return tuple(out)
 
 
@@ -522,13 +529,11 @@ def token_logprobs(logits_last, logits_suf, tokens, cu_prefix, cu_suffix, group_
         workspace = torch.empty(token_logprobs_workspace_bytes(ng, ns, ts, vocab), device=dev, dtype=torch.uint8)
     _expect(dev, None, **{n: ((ts,), t) for n, t in zip(("logp", "lse", "entropy"), out[:3 if entropy else 2])})
     _workspace(workspace, dev)
-    with torch.cuda.device(dev):
-        st = lib().pg_token_logprobs(
-            _dtype_code(torch, logits_suf.dtype), tokens.element_size(), ng, ns, int(total_prefix), ts,
-            _ptr(cu_prefix), _ptr(cu_suffix), _ptr(group_sizes), vocab, float(temperature), _ptr(logits_last),
-            _row_stride(logits_last), _ptr(logits_suf), _row_stride(logits_suf), _ptr(tokens), _ptr(out[0]),
-            _ptr(out[1]), _ptr(out[2]) if entropy else None, _ptr(workspace), workspace.numel(), _stream(torch, dev))
-    _check(st)
+    _launch(
+        dev, lib().pg_token_logprobs, _dtype_code(torch, logits_suf.dtype), tokens.element_size(), ng, ns,
+        int(total_prefix), ts, _ptr(cu_prefix), _ptr(cu_suffix), _ptr(group_sizes), vocab, float(temperature),
+        _ptr(logits_last), _row_stride(logits_last), _ptr(logits_suf), _row_stride(logits_suf), _ptr(tokens),
+        _ptr(out[0]), _ptr(out[1]), _ptr(out[2]) if entropy else None, _ptr(workspace), workspace.numel())
     return tuple(out[:3 if entropy else 2])
 
 
@@ -546,14 +551,11 @@ def token_logprobs_bwd(logits_last, logits_suf, tokens, lse, dlogp, cu_prefix, c
     _expect(dev, None, lse=((ts,), lse), dlogp=((ts,), dlogp))
     _logit_rows(dev, dt, dlogits_last=((ng, vocab), out[0]), dlogits_suf=((ts, vocab), out[1]))
     _workspace(workspace, dev)
-    with torch.cuda.device(dev):
-        st = lib().pg_token_logprobs_bwd(
-            _dtype_code(torch, dt), tokens.element_size(), ng, ns, int(total_prefix), ts, _ptr(cu_prefix),
-            _ptr(cu_suffix), _ptr(group_sizes), vocab, float(temperature), _ptr(logits_last), _row_stride(logits_last),
-            _ptr(logits_suf), _row_stride(logits_suf), _ptr(tokens), _ptr(lse), _ptr(dlogp), _ptr(out[0]),
-            _row_stride(out[0]), _ptr(out[1]), _row_stride(out[1]), _ptr(workspace), workspace.numel(),
-            _stream(torch, dev))
-    _check(st)
+    _launch(
+        dev, lib().pg_token_logprobs_bwd, _dtype_code(torch, dt), tokens.element_size(), ng, ns, int(total_prefix),
+        ts, _ptr(cu_prefix), _ptr(cu_suffix), _ptr(group_sizes), vocab, float(temperature), _ptr(logits_last),
+        _row_stride(logits_last), _ptr(logits_suf), _row_stride(logits_suf), _ptr(tokens), _ptr(lse), _ptr(dlogp),
+        _ptr(out[0]), _row_stride(out[0]), _ptr(out[1]), _row_stride(out[1]), _ptr(workspace), workspace.numel())
     return tuple(out)
 
 
@@ -589,12 +591,10 @@ def policy_loss(logp, advantages, cu_suffix, group_sizes, logp_old=None, logp_re
         _expect(dev, mask.dtype, mask=((ts,), mask))
     _grouping(dev, cu_suffix=(ns + 1, cu_suffix), group_sizes=(ng, group_sizes))
     _workspace(workspace, dev)
-    with torch.cuda.device(dev):
-        st = lib().pg_policy_loss(
-            AVERAGES[average], ng, ns, ts, _ptr(cu_suffix), _ptr(group_sizes), float(clip[0]), float(clip[1]),
-            float(beta), float(grad_scale), _ptr(logp), _ptr(logp_old), _ptr(logp_ref), _ptr(advantages), _ptr(mask),
-            _ptr(out[0]), _ptr(out[1]), _ptr(workspace), workspace.numel(), _stream(torch, dev))
-    _check(st)
+    _launch(
+        dev, lib().pg_policy_loss, AVERAGES[average], ng, ns, ts, _ptr(cu_suffix), _ptr(group_sizes),
+        float(clip[0]), float(clip[1]), float(beta), float(grad_scale), _ptr(logp), _ptr(logp_old), _ptr(logp_ref),
+        _ptr(advantages), _ptr(mask), _ptr(out[0]), _ptr(out[1]), _ptr(workspace), workspace.numel())
     return tuple(out)
 
 

@@ -49,6 +49,7 @@ struct LinArgs {
   const GroupInfoEx* ginfo;
   int ng, ns, h_q, h_kv, max_items;
   int l_pre, l_suf;   // rows of a prefix's and of a member's items
+  int alone;          // no states between items: a workgroup walks what its own starts from
   int members_first;  // backward: the members' gradients are done before the prefixes' walk starts
   float scale;
 };
@@ -232,9 +233,10 @@ struct RowDecay {
       in_step[s] = fast_exp2(g * (float)(REV ? row : 15 - row));
     }
   }
-  __device__ __forceinline__ void step(int t, int n, float (&w)[8]) const {
+  // before (backward): rows of the segment in front of the chunk, whose decay is not in the state yet
+  __device__ __forceinline__ void step(int t, int n, float (&w)[8], int before) const {
     if (REV || 16 * t + 16 <= n) {
-      const float f = fast_exp2(g * (float)(REV ? 16 * t : n - 16 - 16 * t));
+      const float f = fast_exp2(g * (float)(REV ? before + 16 * t : n - 16 - 16 * t));
 #pragma unroll
       for (int s = 0; s < 8; ++s) w[s] = f * in_step[s];
     } else {  // the step that the chunk ends in: its rows past the end are zero
@@ -244,17 +246,17 @@ struct RowDecay {
   }
 };
 
-// acc[kb] += sum over the chunk's n rows of a_row^T (l^e(row) b_row): a's columns 32 (kb0 + kb).., b's columns 32 nb.. .
+// acc[kb] += sum over the chunk's n rows of a_row^T (l^e(row) b_row) (backward: e + before): a's columns 32 (kb0 + kb).., b's columns 32 nb.. .
 template <typename T, int D, int C, bool REV, int SPLIT, int N>
 __device__ __forceinline__ void state_update(f32x16 (&acc)[N], const char* ta, const char* tb,
                                              const FragOffsets<T, D>& fo, const RowDecay<REV>& rd, int kb0, int nb,
-                                             int n) {
+                                             int n, int before = 0) {
   using E = Elt<T>;
 #pragma unroll
   for (int t = 0; t < C / 16; ++t) {
     if (t > 0 && 16 * t >= n) break;
     float w[8], x[8];
-    rd.step(t, n, w);
+    rd.step(t, n, w, before);
     const typename E::Frag b = fo.tr(tb, t, nb);
 #pragma unroll
     for (int s = 0; s < 8; ++s) x[s] = E::frag_elem(b, s) * w[s];
@@ -397,8 +399,8 @@ __device__ __forceinline__ void tile_to_memory(const TileLoader<T, ROWS, D, NT>&
 template <int D>
 __device__ __forceinline__ const float* state_before(const LinArgs& a, const LinItem& it, int kv, bool reverse) {
   const size_t per = (size_t)D * D;
-  if (it.prev >= 0) return a.slots + ((size_t)it.prev * a.h_kv + kv) * per;
-  if (it.prev == kNoState) return nullptr;
+  if (it.prev >= 0 && !a.alone) return a.slots + ((size_t)it.prev * a.h_kv + kv) * per;
+  if (it.prev == kNoState || (a.alone && reverse)) return nullptr;
   if (reverse) return a.slots + ((size_t)(a.max_items + it.group) * a.h_kv + kv) * per;
   return a.state_in ? a.state_in + ((size_t)it.group * a.h_kv + kv) * per : nullptr;
 }
@@ -606,6 +608,21 @@ __global__ void __launch_bounds__(kLinThreads, sizeof(T) == 2 ? 2 : 1) lin_out_k
   auto load_q = [&](int done, int r) {
     lq.load(nullptr, q + ((size_t)(it.row0 + done) * a.h_q + h0 + r) * D, gq, min(S::kC, it.nrows - done));
   };
+  if (a.alone && it.part) {  // a member: its group's prefix first
+    const T *pk = (const T*)a.k[0], *pv = (const T*)a.v[0];
+    const int p0 = uniform(a.cu_p[it.group]), p1 = uniform(a.cu_p[it.group + 1]);
+    for (int r = p0; r < p1; r += S::kC) {
+      const int n = min(S::kC, p1 - r);
+      lk.load(nullptr, pk + ((size_t)r * a.h_kv + kv) * D, gs, n);
+      lv.load(nullptr, pv + ((size_t)r * a.h_kv + kv) * D, gs, n);
+      __syncthreads();
+      lk.store(tk);
+      lv.store(tv);
+      __syncthreads();
+      state_scale(acc, fast_exp2(g * (float)n));
+      state_update<T, D, S::kC, false, SPLIT>(acc, tk, tv, fo, rd, kb0, nb, n);
+    }
+  }
   load_kv(0);
   load_q(0, 0);
   for (int done = 0; done < it.nrows; done += S::kC) {
@@ -722,6 +739,26 @@ __global__ void __launch_bounds__(kLinThreads, sizeof(T) == 2 ? 2 : 1) lin_grad_
     lq.load(nullptr, q + at, gq, rows(done));
     ld.load(nullptr, d_o + at, gq, rows(done));
   };
+  if (a.alone && !it.part) {  // a prefix: its members' rows first, each by its distance from the prefix's end
+    const T *sq = (const T*)a.q[1], *sd = (const T*)a.d_o[1];
+    const int m0 = uniform(a.ginfo[it.group].m0), m1 = uniform(a.ginfo[it.group].m1);
+    for (int m = m0; m < m1; ++m) {
+      const int r0 = uniform(a.cu_s[m]), r1 = uniform(a.cu_s[m + 1]);
+      for (int r = r0; r < r1; r += S::kC)
+        for (int j = 0; j < ratio; ++j) {
+          const int n = min(S::kC, r1 - r);
+          const size_t at = ((size_t)r * a.h_q + kv * ratio + j) * D;
+          lq.load(nullptr, sq + at, gq, n);
+          ld.load(nullptr, sd + at, gq, n);
+          __syncthreads();
+          lq.store(tq);
+          ld.store(tdo);
+          __syncthreads();
+          state_update<T, D, S::kC, true, SPLIT>(acc, tq, tdo, fo, rd, kb0, nb, n, r - r0);
+        }
+    }
+    __syncthreads();
+  }
   load_kv(0);
   load_q(0, 0);
   for (int done = 0; done < it.nrows; done += S::kC) {

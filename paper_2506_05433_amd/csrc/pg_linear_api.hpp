@@ -10,28 +10,54 @@ struct ItemRows {
   int pre, suf;
   int hpw;  // query heads a workgroup of the output kernel takes
   bool members_first;
+  bool alone;  // no states between workgroups: each walks the rows that its own start from as well
   int round;  // items that fill the CUs once, where they are ordered by length (pg_linear.hpp, item_place)
 };
 
-ItemRows linear_item_rows(int ns, int tp, int ts, int h_q, int h_kv, bool grad) {
+// Few rows are launches and latency: the state and scan kernels of both walks are 9 of a step's 14 launches. Where one
+// workgroup gets over the rows that its own start from faster than those kernels pass it the state, every segment is
+// one item, and a member's workgroup walks its prefix first (a prefix's its members, backwards). Measured, us alone
+// and in 32-row items, forward then backward: P 64, 4 x 24 rows, d 64, fp32 16, 22 and 35, 45; bf16 P 128, 4 x 16,
+// 8/2 heads 16, 20 and (dk, dv walk 192 rows x 4 heads) 54, 43; P 192 20, 21 and 81, 47; P 400 33, 23; fp32 d 128
+// P 128 36, 25.
+constexpr int kAloneRows = 512;
+
+bool linear_alone(int dtype, int tp, int ts, int ratio, int d, bool grad) {
+  const long rows = (long)tp + ts;
+  if (rows > kAloneRows) return false;
+  return grad ? rows * ratio <= 384 : (long)tp * d <= (dtype == PG_BF16 ? 128 * 128 : 64 * 128);
+}
+
+ItemRows linear_item_rows(int ns, int tp, int ts, int h_q, int h_kv, int d, bool grad, bool alone) {
   ItemRows r{};
   const int ratio = h_kv > 0 ? h_q / h_kv : 1;
   const long rows = (long)tp + ts;
   r.hpw = 1;
+  if (alone) {
+    r.pre = r.suf = kAloneRows + 1;  // no segment is longer: no more items than segments
+    r.alone = true;
+    return r;
+  }
+  // output workgroups take all query heads of a kv head (or a divisor of their number) while there are 512 of them
+  // with 128-row items: they share the state's updates, keys and values. P 4096, 8 x 256..1024 rows, 32/8 heads: 1, 2
+  // and 4 heads 79, 57 and 52 us
   if (!grad)
-    for (int d = 1; d <= ratio; ++d)
-      if (ratio % d == 0 && rows * h_kv * (ratio / d) >= 512L * 128) r.hpw = d;
+    for (int n = 1; n <= ratio; ++n)
+      if (ratio % n == 0 && rows * h_kv * (ratio / n) >= 512L * 128) r.hpw = n;
   const int heads = grad ? h_kv : h_q / r.hpw;
-  // prefixes: enough items to fill the CUs with state workgroups (one a kv head) and output workgroups
+  // prefixes: enough items to fill the CUs with state workgroups (one a kv head); a chunk at least. P 16384 of 8 kv
+  // heads, 256, 512 and 1024 rows: forward state and output 29 + 111, 27 + 110, 38 + 187 us, backward 99 + 152,
+  // 81 + 157, 112 + 257; P 400 of 2, backward as a whole with 32, 64, 128 and 256 rows: 47, 55, 77 and 123 us
+  const int least = d == 128 ? 32 : 64;
   r.pre = 1024;
-  while (r.pre > 128 && (long)tp * h_kv < 256L * r.pre) r.pre /= 2;
+  while (r.pre > least && (long)tp * h_kv < 256L * r.pre) r.pre /= 2;
   // members: whole where there are enough of them (up to twice the mean length: a longer one is split), else as prefixes
   const bool many = (long)ns * heads >= 512;
   r.suf = 1024;
   if (many)
     while (r.suf < 65536 && (long)r.suf * ns < 2L * ts) r.suf *= 2;
   else
-    while (r.suf > 128 && rows * heads < 512L * r.suf) r.suf /= 2;
+    while (r.suf > least && rows * heads < 512L * r.suf) r.suf /= 2;
   r.members_first = many;
   r.round = many ? (int)ceil_div_l(256, heads) : 0;
   return r;
@@ -47,7 +73,9 @@ struct LinearLayout {
   List out, grad;  // the forward walk (outputs, or dq); the backward one (dk, dv)
 };
 
-LinearLayout linear_layout(int ng, int ns, int tp, int ts, int h_q, int h_kv, int d, bool bwd) {
+// dtype: PG_BF16 or PG_FP32, or -1 for a layout that serves both, and a call that returns states (which the scans write
+// for segments without rows); it is the largest.
+LinearLayout linear_layout(int dtype, int ng, int ns, int tp, int ts, int h_q, int h_kv, int d, bool bwd) {
   LinearLayout L{};
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
@@ -57,7 +85,8 @@ LinearLayout linear_layout(int ng, int ns, int tp, int ts, int h_q, int h_kv, in
   L.kvoff = take(sizeof(int) * ((size_t)ng + 1));
   long most = 0;
   auto list = [&](LinearLayout::List& l, bool grad) {
-    l.rows = linear_item_rows(ns, tp, ts, h_q, h_kv, grad);
+    const bool alone = dtype >= 0 && linear_alone(dtype, tp, ts, h_q / h_kv, d, grad);
+    l.rows = linear_item_rows(ns, tp, ts, h_q, h_kv, d, grad, alone);
     // a segment of r rows has ceil(r / rows of an item) items
     const long items = (long)tp / l.rows.pre + ng + (long)ts / l.rows.suf + ns;
     l.max_items = items > INT32_MAX ? -1 : (int)items;
@@ -117,7 +146,7 @@ void linear_states(const Common& c, const pg::LinArgs& a, hipStream_t st) {
 // The forward walk: shares, scans (prefixes, then the members that start from them), outputs.
 template <typename T, int D, int SPLIT>
 void linear_walk(const Common& c, int hpw, const pg::LinArgs& a, hipStream_t st) {
-  {
+  if (!a.alone) {
     Timed tm(PG_K_LINEAR_STATE, st);
     linear_states<T, D, false, SPLIT>(c, a, st);
     linear_scan<D, false, 0>(c, a, st);
@@ -143,6 +172,7 @@ void linear_common_args(pg::LinArgs& a, const Common& c, const LinearLayout& L, 
   a.ng = c.ng; a.ns = c.ns; a.h_q = c.h_q; a.h_kv = c.h_kv; a.max_items = l.max_items;
   a.l_pre = l.rows.pre; a.l_suf = l.rows.suf;
   a.members_first = l.rows.members_first;
+  a.alone = l.rows.alone;
   a.scale = c.scale;
 }
 
@@ -162,7 +192,7 @@ void linear_bwd_typed(const Common& c, int hpw, const pg::LinArgs& dq, const pg:
     const long blocks = pg::xcd_grid_blocks(g.max_items, c.h_kv, 1);
     hipLaunchKernelGGL((pg::lin_grad_kernel<T, D, SPLIT>), dim3((unsigned)blocks), dim3(pg::kLinThreads), 0, st, g, part);
   };
-  {
+  if (!g.alone) {
     Timed tm(PG_K_LINEAR_STATE, st);
     linear_states<T, D, true, SPLIT>(c, g, st);
     linear_scan<D, true, 1>(c, g, st);
@@ -200,14 +230,14 @@ size_t pg_linear_fwd_workspace_size(int n_groups, int n_suffixes, int total_pref
                                     int h_kv, int head_dim) {
   if (n_groups < 0 || n_suffixes < 0 || total_prefix < 0 || total_suffix < 0 || h_q < 0 || h_kv < 0 || head_dim < 0)
     return 0;
-  return linear_layout(n_groups, n_suffixes, total_prefix, total_suffix, h_q, h_kv, head_dim, false).total;
+  return linear_layout(-1, n_groups, n_suffixes, total_prefix, total_suffix, h_q, h_kv, head_dim, false).total;
 }
 
 size_t pg_linear_bwd_workspace_size(int n_groups, int n_suffixes, int total_prefix, int total_suffix, int h_q,
                                     int h_kv, int head_dim) {
   if (n_groups < 0 || n_suffixes < 0 || total_prefix < 0 || total_suffix < 0 || h_q < 0 || h_kv < 0 || head_dim < 0)
     return 0;
-  return linear_layout(n_groups, n_suffixes, total_prefix, total_suffix, h_q, h_kv, head_dim, true).total;
+  return linear_layout(-1, n_groups, n_suffixes, total_prefix, total_suffix, h_q, h_kv, head_dim, true).total;
 }
 
 int pg_linear_fwd(int dtype, int n_groups, int n_suffixes, int total_prefix, int total_suffix,
@@ -225,7 +255,7 @@ int pg_linear_fwd(int dtype, int n_groups, int n_suffixes, int total_prefix, int
   if (total_suffix > 0 && (!q_suf || !k_suf || !v_suf || !o_suf)) return fail(PG_EINVAL, "a suffix tensor pointer is NULL");
   if (misaligned({q_pre, k_pre, v_pre, q_suf, k_suf, v_suf, state_in, o_pre, o_suf, state_pre, state_suf, workspace}))
     return fail(PG_EINVAL, "tensor pointers must be 16-byte aligned");
-  const LinearLayout L = linear_layout(c.ng, c.ns, c.tp, c.ts, c.h_q, c.h_kv, c.d, false);
+  const LinearLayout L = linear_layout(state_pre || state_suf ? -1 : dtype, c.ng, c.ns, c.tp, c.ts, c.h_q, c.h_kv, c.d, false);
   if ((rc = linear_grid_check(c, L.out))) return rc;
   if (!workspace || workspace_bytes < L.total)
     return fail(PG_EWORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, L.total);
@@ -269,7 +299,7 @@ int pg_linear_bwd(int dtype, int n_groups, int n_suffixes, int total_prefix, int
   if (misaligned({q_pre, k_pre, v_pre, q_suf, k_suf, v_suf, do_pre, do_suf, dq_pre, dk_pre, dv_pre, dq_suf, dk_suf,
                   dv_suf, workspace}))
     return fail(PG_EINVAL, "tensor pointers must be 16-byte aligned");
-  const LinearLayout L = linear_layout(c.ng, c.ns, c.tp, c.ts, c.h_q, c.h_kv, c.d, true);
+  const LinearLayout L = linear_layout(dtype, c.ng, c.ns, c.tp, c.ts, c.h_q, c.h_kv, c.d, true);
   if ((rc = linear_grid_check(c, L.out)) || (rc = linear_grid_check(c, L.grad))) return rc;
   if (!workspace || workspace_bytes < L.total)
     return fail(PG_EWORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, L.total);

@@ -439,13 +439,140 @@ struct PolicyArgs {
   double* member_w;  // [n_suffixes]: 1 / (groups * members) of each member
   int* count;        // [n_suffixes + 1]: kept tokens of each member, and of all
   double* part;      // [blocks, 4]
-  unsigned* done;
-  int ng, ns, ts, by_token, blocks;
+  int ng, ns, ts, by_token;
   double cut_lo, cut_hi, beta, grad_scale;
 };
 constexpr int kPolicyThreads = 1024, kPolicyTok = 256;
+constexpr int kPolicyPer = 4;       // tokens a thread
+constexpr int kPolicySmall = 8192;  // tokens that one workgroup takes in one launch
 
-// Checks and per-member weights; one block.
+struct PolicySums {
+  double v[4];
+};
+
+// One kept token: adds to the sums, returns its gradient.
+__device__ __forceinline__ double policy_token(const PolicyArgs& a, double lp, double old, double ref, double adv,
+                                               double w, PolicySums& s) {
+  const double lr = a.logp_old ? lp - old : 0.0;
+  const bool cut = (adv > 0.0 && lr > a.cut_hi) || (adv < 0.0 && lr < a.cut_lo);
+  const double r = exp(cut ? (adv > 0.0 ? a.cut_hi : a.cut_lo) : lr);
+  const double ra = adv == 0.0 ? 0.0 : r * adv;
+  double kl = 0.0, grad = cut ? 0.0 : -ra;
+  if (a.logp_ref) {
+    const double x = ref - lp, em = expm1(x);
+    kl = em - x;
+    if (a.beta != 0.0) grad -= a.beta * em;
+  }
+  s.v[0] += w * ((a.beta != 0.0 ? a.beta * kl : 0.0) - ra);
+  s.v[1] -= w * ra;
+  s.v[2] += w * kl;
+  s.v[3] += cut ? w : 0.0;
+  return grad * w * a.grad_scale;
+}
+
+// Sums over a workgroup of NT threads in a fixed order; every thread gets them.
+template <int NT>
+__device__ __forceinline__ void block_sum4(PolicySums& s, double (*tmp)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) s.v[k] += __shfl_xor(s.v[k], off);
+    if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6][k] = s.v[k];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    double x = 0.0;
+    for (int w = 0; w < NT / 64; ++w) x += tmp[w][k];
+    s.v[k] = x;
+  }
+}
+
+// Counts the kept tokens of a wave's lanes (whole numbers: their order does not matter); all lanes of the wave come.
+__device__ __forceinline__ void policy_count(bool on, int m, int* count) {
+  const unsigned long long all = __ballot(on);
+  if (__all(m == uniform(m))) {
+    if ((threadIdx.x & 63) == 0 && all) atomicAdd(&count[m], __popcll(all));
+  } else if (on) {
+    atomicAdd(&count[m], 1);
+  }
+}
+
+// The whole loss in one workgroup and launch, for few tokens and grouping arrays that fit LDS: five thousand tokens are
+// launches and dependent loads, no work.
+__global__ void __launch_bounds__(kPolicyThreads) policy_small_kernel(const PolicyArgs a) {
+  __shared__ int cu[kLdsMembers + 1], cnt[kLdsMembers + 1];
+  __shared__ double mw[kLdsMembers], tmp[kPolicyThreads / 64][4];
+  __shared__ int tot[1][kPlanThreads / 64];
+  __shared__ int bad, groups;
+  const int t = threadIdx.x;
+  constexpr int kPer = kPolicySmall / kPolicyThreads;
+  const int size = t < a.ng ? a.gsz[t] : 0;
+  // the tokens are on their way while the grouping arrays are looked over
+  float lp[kPer], old[kPer], ref[kPer];
+  bool on[kPer];
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int i = t + k * kPolicyThreads;
+    on[k] = i < a.ts && (!a.mask || a.mask[i]);
+    lp[k] = i < a.ts ? a.logp[i] : 0.f;
+    old[k] = i < a.ts && a.logp_old ? a.logp_old[i] : 0.f;
+    ref[k] = i < a.ts && a.logp_ref ? a.logp_ref[i] : 0.f;
+  }
+  for (int m = t; m <= a.ns; m += kPolicyThreads) {
+    cu[m] = a.cu_s[m];
+    cnt[m] = 0;
+  }
+  if (t == 0) {
+    bad = 0;
+    groups = 0;
+  }
+  __syncthreads();
+  int b = size < 0 || size > a.ns;
+  for (int m = t; m <= a.ns; m += kPolicyThreads) {
+    const int v = cu[m];
+    if ((m == 0 && v != 0) || (m == a.ns && v != a.ts) || (m > 0 && v < cu[m - 1])) b = 1;
+  }
+  int start[1] = {b ? 0 : size};
+  const int members = start[0];
+  if (members > 0) atomicAdd(&groups, 1);
+  block_exclusive_sums(start, a.ng, tot);  // fits 32 bits: at most kLdsGroups sizes of at most kLdsMembers
+  if (t <= a.ng && ((t == a.ng && start[0] != a.ns) || start[0] + members > a.ns)) b = 1;
+  if (b) atomicOr(&bad, 1);
+  __syncthreads();
+  if (t == 0) a.hdr->error = bad;
+  if (bad) return;
+  for (int m = start[0]; m < start[0] + members; ++m) mw[m] = (double)groups * (double)members;
+  int mem[kPer];
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int i = t + k * kPolicyThreads;
+    mem[k] = i < a.ts ? upper_index(cu, 0, a.ns, i) : 0;
+    if (a.mask && i - (t & 63) < a.ts) policy_count(on[k], a.by_token ? a.ns : mem[k], cnt);  // whole waves
+  }
+  if (!a.mask)
+    for (int m = t; m <= a.ns; m += kPolicyThreads) cnt[m] = m < a.ns ? cu[m + 1] - cu[m] : a.ts;
+  __syncthreads();
+  for (int m = t; m < a.ns; m += kPolicyThreads) mw[m] = 1.0 / (a.by_token ? (double)cnt[a.ns] : mw[m] * cnt[m]);
+  __syncthreads();
+  PolicySums s{{0.0, 0.0, 0.0, 0.0}};
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int i = t + k * kPolicyThreads;
+    if (i >= a.ts) break;
+    double g = 0.0;
+    if (on[k]) {
+      g = policy_token(a, lp[k], old[k], ref[k], a.adv[mem[k]], mw[mem[k]], s);
+    }
+    if (a.dlogp) a.dlogp[i] = (float)g;
+  }
+  block_sum4<kPolicyThreads>(s, tmp);
+  if (t == 0)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) a.stats[k] = (float)s.v[k];
+}
+
+// Otherwise three launches, four with a mask. Checks and per-member weights; one block.
 __global__ void __launch_bounds__(kPolicyThreads) policy_plan_kernel(const PolicyArgs a) {
   __shared__ long long tmp[kPolicyThreads];
   __shared__ long long members;
@@ -459,9 +586,12 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_plan_kernel(const Polic
   __syncthreads();
   int b = 0;
   for (int m = t; m <= a.ns; m += kPolicyThreads) {
-    const int v = a.cu_s[m];
-    if ((m == 0 && v != 0) || (m == a.ns && v != a.ts) || (m > 0 && v < a.cu_s[m - 1])) b = 1;
+    const int v = a.cu_s[m], before = m > 0 ? a.cu_s[m - 1] : 0;
+    if ((m == 0 && v != 0) || (m == a.ns && v != a.ts) || v < before) b = 1;
+    if (a.mask) a.count[m] = 0;
+    else if (m > 0) a.count[m - 1] = v - before;
   }
+  if (t == 0 && !a.mask) a.count[a.ns] = a.ts;
   int full = 0;
   for (int g = t; g < a.ng; g += kPolicyThreads) {
     const int v = a.gsz[g];
@@ -481,101 +611,114 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_plan_kernel(const Polic
     if (t == kPolicyThreads - 1) members = end;
     __syncthreads();
   }
-  for (int m = t; m <= a.ns; m += kPolicyThreads)
-    a.count[m] = a.mask || bad ? 0 : m < a.ns ? a.cu_s[m + 1] - a.cu_s[m] : a.ts;
   if (t == 0) {
     a.hdr->error = bad || members != a.ns;
-    *a.done = 0;
   }
 }
 
-// Kept tokens of each member (whole numbers: their order does not matter).
+// The member of token i, whose workgroup's tokens lie in members m0 .. m1.
+__device__ __forceinline__ int policy_member(const PolicyArgs& a, int m0, int m1, int i) {
+  return upper_index(a.cu_s, m0, m1 + 1, i);
+}
+
+// Kept tokens of each member, or of all. One atomic a wave where its lanes are in one member: an atomic for each wave
+// of 64 tokens on one counter was 52 of 94 us at 266k tokens.
 __global__ void __launch_bounds__(kPolicyTok) policy_count_kernel(const PolicyArgs a) {
+  __shared__ int sum;
   if (a.hdr->error) return;
-  const long i = (long)blockIdx.x * kPolicyTok + threadIdx.x;
-  const bool on = i < a.ts && a.mask[i];
-  const int m = i < a.ts ? upper_index(a.cu_s, 0, a.ns, (int)i) : -1;
-  const int m0 = uniform(m);
-  const unsigned long long all = __ballot(on);
-  if ((threadIdx.x & 63) == 0 && all) atomicAdd(&a.count[a.ns], __popcll(all));
-  if (__all(m == m0 || m < 0)) {
-    if ((threadIdx.x & 63) == 0 && all) atomicAdd(&a.count[m0], __popcll(all));
-  } else if (on) {
-    atomicAdd(&a.count[m], 1);
-  }
-}
-
-struct PolicySums {
-  double v[4];
-};
-__device__ __forceinline__ void policy_token(const PolicyArgs& a, int i, int m, double w, PolicySums& s) {
-  const bool on = !a.mask || a.mask[i];
-  double grad = 0.0;
-  if (on) {
-    const double lp = a.logp[i], adv = a.adv[m];
-    const double lr = a.logp_old ? lp - (double)a.logp_old[i] : 0.0;
-    const bool cut = (adv > 0.0 && lr > a.cut_hi) || (adv < 0.0 && lr < a.cut_lo);
-    const double r = exp(cut ? (adv > 0.0 ? a.cut_hi : a.cut_lo) : lr);
-    const double ra = adv == 0.0 ? 0.0 : r * adv;
-    double kl = 0.0;
-    grad = cut ? 0.0 : -ra;
-    if (a.logp_ref) {
-      const double x = (double)a.logp_ref[i] - lp, em = expm1(x);
-      kl = em - x;
-      if (a.beta != 0.0) grad -= a.beta * em;
+  const int t = threadIdx.x;
+  const long first = (long)blockIdx.x * kPolicyTok * kPolicyPer;
+  const int last = (int)min((long)a.ts, first + kPolicyTok * kPolicyPer) - 1;
+  if (a.by_token) {
+    if (t == 0) sum = 0;
+    __syncthreads();
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < kPolicyPer; ++k) {
+      const long i = first + t + k * kPolicyTok;
+      n += __popcll(__ballot(i <= last && a.mask[i]));
     }
-    s.v[0] += w * ((a.beta != 0.0 ? a.beta * kl : 0.0) - ra);
-    s.v[1] -= w * ra;
-    s.v[2] += w * kl;
-    s.v[3] += cut ? w : 0.0;
-    grad *= w * a.grad_scale;
+    if ((t & 63) == 0) atomicAdd(&sum, n);
+    __syncthreads();
+    if (t == 0) atomicAdd(&a.count[a.ns], sum);
+    return;
   }
-  if (a.dlogp) a.dlogp[i] = (float)grad;
-}
-
-__device__ __forceinline__ double policy_weight(const PolicyArgs& a, int m) {
-  const int n = a.count[a.by_token ? a.ns : m];
-  return n == 0 ? 0.0 : a.by_token ? 1.0 / n : a.member_w[m] / n;
-}
-
-template <int NT>
-__device__ __forceinline__ void block_sum4(PolicySums& s, double (*tmp)[4]) {
+  const int m0 = wave_upper_index(a.cu_s, a.ns, (int)first), m1 = wave_upper_index(a.cu_s, a.ns, last);
+  if (m0 == m1) {
+    if (t == 0) sum = 0;
+    __syncthreads();
+    int n = 0;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) s.v[k] += __shfl_xor(s.v[k], off);
-    if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6][k] = s.v[k];
+    for (int k = 0; k < kPolicyPer; ++k) {
+      const long i = first + t + k * kPolicyTok;
+      n += __popcll(__ballot(i <= last && a.mask[i]));
+    }
+    if ((t & 63) == 0) atomicAdd(&sum, n);
+    __syncthreads();
+    if (t == 0) atomicAdd(&a.count[m0], sum);
+    return;
   }
-  __syncthreads();
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    double x = 0.0;
-    for (int w = 0; w < NT / 64; ++w) x += tmp[w][k];
-    s.v[k] = x;
+  for (int k = 0; k < kPolicyPer; ++k) {
+    const long i = first + t + k * kPolicyTok;
+    policy_count(i <= last && a.mask[i], policy_member(a, m0, m1, (int)min(i, (long)last)), a.count);
   }
 }
 
+// Terms, gradients and each workgroup's sums.
 __global__ void __launch_bounds__(kPolicyTok) policy_loss_kernel(const PolicyArgs a) {
+  __shared__ double tmp[kPolicyTok / 64][4];
+  const int t = threadIdx.x;
+  const long first = (long)blockIdx.x * kPolicyTok * kPolicyPer;
+  const int last = (int)min((long)a.ts, first + kPolicyTok * kPolicyPer) - 1;
+  PolicySums s{{0.0, 0.0, 0.0, 0.0}};
+  if (first <= last) {
+    float lp[kPolicyPer], old[kPolicyPer], ref[kPolicyPer];
+    bool on[kPolicyPer];
+#pragma unroll
+    for (int k = 0; k < kPolicyPer; ++k) {
+      const long i = min(first + t + k * kPolicyTok, (long)last);
+      on[k] = first + t + k * kPolicyTok <= last && (!a.mask || a.mask[i]);
+      lp[k] = a.logp[i];
+      old[k] = a.logp_old ? a.logp_old[i] : 0.f;
+      ref[k] = a.logp_ref ? a.logp_ref[i] : 0.f;
+    }
+    const int m0 = wave_upper_index(a.cu_s, a.ns, (int)first), m1 = wave_upper_index(a.cu_s, a.ns, last);
+    if (a.hdr->error) return;  // whole workgroups; what is above stays in bounds whatever the arrays hold
+    auto weight = [&](int m) { return a.by_token ? 1.0 / a.count[a.ns] : a.member_w[m] / a.count[m]; };
+    const bool one = m0 == m1 || a.by_token;  // one weight for all
+    const double w0 = one ? weight(m0) : 0.0;
+#pragma unroll
+    for (int k = 0; k < kPolicyPer; ++k) {
+      const long i = first + t + k * kPolicyTok;
+      double g = 0.0;
+      if (on[k]) {
+        const int m = policy_member(a, m0, m1, (int)i);
+        g = policy_token(a, lp[k], old[k], ref[k], a.adv[m], one ? w0 : weight(m), s);
+      }
+      if (a.dlogp && i <= last) a.dlogp[i] = (float)g;
+    }
+  }
+  if (a.hdr->error) return;
+  block_sum4<kPolicyTok>(s, tmp);
+  if (t == 0)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) a.part[4 * (size_t)blockIdx.x + k] = s.v[k];
+}
+
+// The workgroups' sums, in their order. A launch of its own: that the last workgroup of the kernel above adds them up
+// would need each to flush its XCD's L2 (266k tokens: 18 and 25 us with 260 and 521 workgroups, 12 us without).
+__global__ void __launch_bounds__(kPolicyTok) policy_sum_kernel(const PolicyArgs a, int blocks) {
   __shared__ double tmp[kPolicyTok / 64][4];
   if (a.hdr->error) return;
   PolicySums s{{0.0, 0.0, 0.0, 0.0}};
-  for (long i = (long)blockIdx.x * kPolicyTok + threadIdx.x; i < a.ts; i += (long)gridDim.x * kPolicyTok) {
-    const int m = upper_index(a.cu_s, 0, a.ns, (int)i);
-    policy_token(a, (int)i, m, policy_weight(a, m), s);
-  }
-  block_sum4<kPolicyTok>(s, tmp);
-  if (threadIdx.x < 4) a.part[4 * blockIdx.x + threadIdx.x] = s.v[threadIdx.x];
-}
-
-// The blocks' sums, in block order.
-__global__ void __launch_bounds__(64) policy_sum_kernel(const PolicyArgs a) {
-  if (a.hdr->error) return;
-  double x = 0.0;
-  const int k = threadIdx.x & 3;
-  for (int b = threadIdx.x >> 2; b < a.blocks; b += 16) x += a.part[4 * b + k];
+  for (int b = threadIdx.x; b < blocks; b += kPolicyTok)
 #pragma unroll
-  for (int off = 32; off >= 4; off >>= 1) x += __shfl_xor(x, off);
-  if (threadIdx.x < 4) a.stats[threadIdx.x] = (float)x;
+    for (int k = 0; k < 4; ++k) s.v[k] += a.part[4 * (size_t)b + k];
+  block_sum4<kPolicyTok>(s, tmp);
+  if (threadIdx.x == 0)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) a.stats[k] = (float)s.v[k];
 }
 
 }  // namespace pg

@@ -53,20 +53,19 @@ int run_logprobs(int dtype, const pg::LogprobArgs& a0, bool bwd, const int32_t* 
 }
 
 struct PolicyLayout {
-  size_t hdr, member_w, count, part, done, total;
+  size_t hdr, member_w, count, part, total;
   int blocks;
 };
 
 PolicyLayout policy_layout(int ns, int ts) {
   PolicyLayout L{};
-  L.blocks = (int)std::max(1L, std::min(1024L, ceil_div_l(ts, pg::kPolicyTok)));
+  L.blocks = (int)std::max(1L, ceil_div_l(ts, pg::kPolicyTok * pg::kPolicyPer));
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
   L.hdr = take(sizeof(pg::PlanHeader));
   L.member_w = take(sizeof(double) * (size_t)(ns > 0 ? ns : 1));
   L.count = take(sizeof(int) * ((size_t)ns + 1));
   L.part = take(sizeof(double) * 4 * (size_t)L.blocks);
-  L.done = take(sizeof(unsigned));
   L.total = off;
   return L;
 }
@@ -173,11 +172,14 @@ int pg_policy_loss(int average, int n_groups, int n_suffixes, int total_suffix, 
   a.member_w = (double*)(ws + L.member_w);
   a.count = (int*)(ws + L.count);
   a.part = (double*)(ws + L.part);
-  a.done = (unsigned*)(ws + L.done);
   a.ng = n_groups; a.ns = n_suffixes; a.ts = total_suffix; a.by_token = average == PG_AVERAGE_TOKEN;
-  a.blocks = L.blocks;
   a.cut_lo = std::log1p(-clip_low); a.cut_hi = std::log1p(clip_high);
   a.beta = beta; a.grad_scale = grad_scale;
+  if (total_suffix <= pg::kPolicySmall && pg::plan_fits_lds(n_groups, n_suffixes)) {
+    Timed tm(PG_K_POLICY, st);
+    hipLaunchKernelGGL(pg::policy_small_kernel, dim3(1), dim3(pg::kPolicyThreads), 0, st, a);
+    return finish_plan(a.hdr, st);
+  }
   {
     Timed tp(PG_K_PLAN, st);
     hipLaunchKernelGGL(pg::policy_plan_kernel, dim3(1), dim3(pg::kPolicyThreads), 0, st, a);
@@ -185,10 +187,9 @@ int pg_policy_loss(int average, int n_groups, int n_suffixes, int total_suffix, 
   }
   Timed tm(PG_K_POLICY, st);
   if (mask && total_suffix > 0)
-    hipLaunchKernelGGL(pg::policy_count_kernel, dim3((unsigned)ceil_div_l(total_suffix, pg::kPolicyTok)),
-                       dim3(pg::kPolicyTok), 0, st, a);
+    hipLaunchKernelGGL(pg::policy_count_kernel, dim3((unsigned)L.blocks), dim3(pg::kPolicyTok), 0, st, a);
   hipLaunchKernelGGL(pg::policy_loss_kernel, dim3((unsigned)L.blocks), dim3(pg::kPolicyTok), 0, st, a);
-  hipLaunchKernelGGL(pg::policy_sum_kernel, dim3(1), dim3(64), 0, st, a);
+  hipLaunchKernelGGL(pg::policy_sum_kernel, dim3(1), dim3(pg::kPolicyTok), 0, st, a, L.blocks);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "policy loss launch");
   return PG_OK;
