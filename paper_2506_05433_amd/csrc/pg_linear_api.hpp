@@ -39,25 +39,29 @@ ItemRows linear_item_rows(int ns, int tp, int ts, int h_q, int h_kv, int d, bool
     return r;
   }
   // output workgroups take all query heads of a kv head (or a divisor of their number) while there are 512 of them
-  // with 128-row items: they share the state's updates, keys and values. P 4096, 8 x 256..1024 rows, 32/8 heads: 1, 2
-  // and 4 heads 79, 57 and 52 us
+  // with 64-row items: they share the state's updates, keys and values. P 4096, 8 x 256..1024 rows, 32/8 heads: 1, 2
+  // and 4 heads 79, 57 and 52 us; 8100 rows, 16/4 heads, d 64: 25, 22 and 18
   if (!grad)
     for (int n = 1; n <= ratio; ++n)
-      if (ratio % n == 0 && rows * h_kv * (ratio / n) >= 512L * 128) r.hpw = n;
+      if (ratio % n == 0 && rows * h_kv * (ratio / n) >= 512L * 64) r.hpw = n;
   const int heads = grad ? h_kv : h_q / r.hpw;
-  // prefixes: enough items to fill the CUs with state workgroups (one a kv head); a chunk at least. P 16384 of 8 kv
-  // heads, 256, 512 and 1024 rows: forward state and output 29 + 111, 27 + 110, 38 + 187 us, backward 99 + 152,
-  // 81 + 157, 112 + 257; P 400 of 2, backward as a whole with 32, 64, 128 and 256 rows: 47, 55, 77 and 123 us
+  // members: whole where there are enough of them (up to twice the mean length: a longer one is split), else about 512
+  // workgroups in all; a chunk at least
   const int least = d == 128 ? 32 : 64;
-  r.pre = 1024;
-  while (r.pre > least && (long)tp * h_kv < 256L * r.pre) r.pre /= 2;
-  // members: whole where there are enough of them (up to twice the mean length: a longer one is split), else as prefixes
   const bool many = (long)ns * heads >= 512;
   r.suf = 1024;
   if (many)
     while (r.suf < 65536 && (long)r.suf * ns < 2L * ts) r.suf *= 2;
   else
     while (r.suf > least && rows * heads < 512L * r.suf) r.suf /= 2;
+  // prefixes: enough items to fill the CUs with the state kernel's workgroups (one a kv head; half the CUs where they
+  // only read keys and values) and, with the members, with the output kernel's. P 16384 of 8 kv heads, 256, 512 and
+  // 1024 rows: forward state and output 29 + 111, 27 + 110, 38 + 187 us, backward 99 + 152, 81 + 157, 112 + 257;
+  // P 4096, 128, 256 and 512: 19 + 52, 16 + 49, 21 + 78; P 400 of 2, a whole backward with 32, 64, 128 and 256: 47, 55,
+  // 77 and 123
+  const long groups = many ? (long)ns * heads : ts / r.suf * heads;
+  r.pre = 1024;
+  while (r.pre > least && ((long)tp * h_kv < (grad ? 256L : 128L) * r.pre || tp / r.pre * heads + groups < 400)) r.pre /= 2;
   r.members_first = many;
   r.round = many ? (int)ceil_div_l(256, heads) : 0;
   return r;
