@@ -456,6 +456,82 @@ def cpu_model():
     return None
 
 
+def _event_ms(torch, call, steps, warmup):
+    """Mean time of a call between HIP events around `steps` of them."""
+    for _ in range(max(warmup, 1)):
+        call()
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    for _ in range(steps):
+        call()
+    b.record()
+    b.synchronize()
+    return a.elapsed_time(b) / steps
+
+
+def time_linear(binding, torch, dev, prob, steps, warmup):
+    """Linear attention with a decay for each kv head on this workload's tensors, forward and backward.
+
+    HBM-bound: the algorithmic traffic reads q, k, v and writes o (forward), reads q, k, v, do and writes dq, dk, dv
+    (backward), every element once.
+    """
+    names = ("q_pre", "k_pre", "v_pre", "q_suf", "k_suf", "v_suf")
+    qkv = [dev[n] for n in names]
+    grp = (dev["cu_prefix"], dev["cu_suffix"], dev["group_sizes"], dev["scale"])
+    decay = -torch.logspace(-4, -0.5, prob.h_kv, device="cuda")
+    o = (torch.empty_like(dev["q_pre"]), torch.empty_like(dev["q_suf"]))
+    g = tuple(torch.empty_like(t) for t in qkv)
+    shape = shape_of(prob)
+    ws = {k: torch.empty(binding.linear_workspace_bytes(k, *shape), device="cuda", dtype=torch.uint8) for k in ("fwd", "bwd")}
+    fwd = _event_ms(torch, lambda: binding.linear_fwd(*qkv, decay, *grp, out=o, workspace=ws["fwd"]), steps, warmup)
+    bwd = _event_ms(torch, lambda: binding.linear_bwd(*qkv, dev["do_pre"], dev["do_suf"], decay, *grp, out=g,
+                                                      workspace=ws["bwd"]), steps, warmup)
+    row = prob.head_dim * (2 if prob.dtype == "bf16" else 4) * (prob.total_prefix + prob.total_suffix)
+    nb = {"fwd": row * 2 * (prob.h_q + prob.h_kv), "bwd": row * (3 * prob.h_q + 4 * prob.h_kv)}
+    del o, g, ws
+    torch.cuda.empty_cache()
+    return {"fwd_ms": round(fwd, 4), "bwd_ms": round(bwd, 4), "fwd_bytes": nb["fwd"], "bwd_bytes": nb["bwd"],
+            "fwd_GBps": round(nb["fwd"] / fwd / 1e6, 1), "bwd_GBps": round(nb["bwd"] / bwd / 1e6, 1), "bound": "hbm"}
+
+
+def time_policy(binding, torch, dev, prob, steps, warmup, vocab=32000):
+    """The end of a GRPO step on this workload's responses: token log-probabilities from bf16 logits, their gradient
+    (in place), and the clipped loss with a KL term between them. The logits are those of the first members, at most
+    32768 rows, the loss runs over all tokens."""
+    import numpy as np
+    cs = np.concatenate([[0], np.cumsum(prob.suffix_lens)])
+    size = int(prob.group_sizes[0])
+    members = int(max(1, min(size, np.searchsorted(cs, 32768, side="right") - 1)))
+    rows, tp = int(cs[members]), int(prob.prefix_lens[0])
+    if rows == 0:
+        return None
+    i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    grp = (i32([0, tp]), i32(cs[:members + 1]), i32([members]))
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    last, suf = (torch.randn(n, vocab, generator=gen, device="cuda").bfloat16() for n in (1, rows))
+    tok = torch.randint(0, vocab, (rows,), generator=gen, device="cuda")
+    ws = torch.empty(binding.token_logprobs_workspace_bytes(1, members, rows, vocab), device="cuda", dtype=torch.uint8)
+    lp = (torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"))
+    f_ms = _event_ms(torch, lambda: binding.token_logprobs(last, suf, tok, *grp, tp, out=lp, workspace=ws), steps, warmup)
+    d = torch.randn(rows, generator=gen, device="cuda") / rows
+    out = (torch.empty_like(last), torch.empty_like(suf))
+    b_ms = _event_ms(torch, lambda: binding.token_logprobs_bwd(last, suf, tok, lp[1], d, *grp, tp, out=out, workspace=ws),
+                     steps, warmup)
+    ts, ns, ng = prob.total_suffix, len(prob.suffix_lens), len(prob.prefix_lens)
+    x = -torch.rand(ts, generator=gen, device="cuda")
+    adv = torch.randn(ns, generator=gen, device="cuda")
+    wp = torch.empty(binding.policy_loss_workspace_bytes(ng, ns, ts), device="cuda", dtype=torch.uint8)
+    res = (torch.empty(4, device="cuda"), torch.empty(ts, device="cuda"))
+    p_ms = _event_ms(torch, lambda: binding.policy_loss(x, adv, dev["cu_suffix"], dev["group_sizes"], logp_old=x, logp_ref=x,
+                                                        beta=0.04, out=res, workspace=wp), steps, warmup)
+    nb = 2 * vocab * (rows - members + 1)
+    del last, suf, out
+    torch.cuda.empty_cache()
+    return {"vocab": vocab, "rows": rows, "logprobs_ms": round(f_ms, 4), "logprobs_GBps": round(nb / f_ms / 1e6, 1),
+            "logprobs_bwd_ms": round(b_ms, 4), "logprobs_bwd_GBps": round(2 * nb / b_ms / 1e6, 1),
+            "policy_tokens": ts, "policy_ms": round(p_ms, 4)}
+
+
 ATTN_SOURCES = ("pg_attn.hip", "pg_bwd.hpp", "pg_bwd_wide.hpp", "pg_common.hpp", "pg_fwd.hpp", "pg_layout.hpp", "pg_plan.hpp",
                 "pg_types.hpp", "pg_wide.hpp")
 
@@ -602,7 +678,7 @@ def main():
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-repeated", action="store_true")
     ap.add_argument("--padded", action="store_true", help="also time the padded layout of Eq. (1)")
-    ap.add_argument("--no-extras", action="store_true", help="skip the rotary-embedding and final-token timings")
+    ap.add_argument("--no-extras", action="store_true", help="skip the timings of the calls beside the attention step")
     ap.add_argument("--cpu-budget", type=float, default=20.0)
     ap.add_argument("--sweep", action="store_true",
                     help="run the paper's Fig. 2/3 grid (one JSON line per point) instead of the bench line")
@@ -682,6 +758,8 @@ def main():
         out["rope"] = time_rope(binding, torch, dev, prob, args.steps, args.warmup)
         out["last"] = time_last(binding, torch, dev, prob, args.steps, args.warmup)
         out["xours"] = time_xours(binding, torch, dev, prob, args.steps, args.warmup, flush, ms)
+        out["linear"] = time_linear(binding, torch, dev, prob, args.steps, args.warmup)
+        out["policy"] = time_policy(binding, torch, dev, prob, args.steps, args.warmup)
     if not args.no_repeated:
         out["speedup_ceiling_pairs"] = round(rep_pairs / pairs, 3)
         G, P, sum_s = prob.group_sizes, prob.prefix_lens, prob.suffix_lens.sum()

@@ -1,7 +1,7 @@
 """Build step for the HIP library (gfx950 only).
 
 ``python -m paper_2506_05433_amd.build`` (or ``build()``) compiles
-``csrc/pg_attn.hip`` with hipcc into ``libpg_attn.so`` next to this file.
+``csrc/pg_lib.hip`` with hipcc into ``libpg_attn.so`` next to this file.
 """
 from __future__ import annotations
 
@@ -11,7 +11,7 @@ import subprocess
 import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = os.path.join(HERE, "csrc", "pg_attn.hip")
+SRC = os.path.join(HERE, "csrc", "pg_lib.hip")
 OUT = os.path.join(HERE, "libpg_attn.so")
 ARCH = "gfx950"
 

@@ -8,7 +8,6 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
-#include <initializer_list>
 #include <mutex>
 #include <string>
 #include <vector>
@@ -18,10 +17,8 @@
 #include "pg_bwd_wide.hpp"
 #include "pg_fwd.hpp"
 #include "pg_layout.hpp"
-#include "pg_linear.hpp"
 #include "pg_plan.hpp"
 #include "pg_last.hpp"
-#include "pg_policy.hpp"
 #include "pg_rope.hpp"
 
 // Scratch of pg_attn_fwd_noalloc: the tile plan that pg_attn_fwd keeps in the caller's
@@ -819,6 +816,3 @@ int pg_grouped_positions(int n_groups, int n_suffixes, int total_prefix, int tot
 }
 
 }  // extern "C"
-
-#include "pg_linear_api.hpp"
-#include "pg_policy_api.hpp"

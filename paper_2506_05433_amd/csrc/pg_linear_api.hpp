@@ -1,4 +1,4 @@
-// Entry points of linear attention (included by pg_attn.hip): argument checks, workspace layout, launches.
+// Entry points of linear attention (included by pg_lib.hip, after the helpers of pg_attn.hip): argument checks, workspace layout, launches.
 #pragma once
 
 namespace {

@@ -179,22 +179,29 @@ __device__ __forceinline__ SoftStat row_stats(const T* x, int vocab, float c, So
     soft_add<ENT>(st, v, c);
   }
   const uint4* xv = (const uint4*)(x + head);
-  int i = t;
-  for (; i + (kUnroll - 1) * NT < nv; i += kUnroll * NT) {
+  for (int i = t; i < nv; i += kUnroll * NT) {
     uint4 u[kUnroll];
+    if (i - t + kUnroll * NT <= nv) {  // the whole workgroup: no test for each piece
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) u[k] = xv[i + k * NT];
+      for (int k = 0; k < kUnroll; ++k) u[k] = xv[i + k * NT];
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-      float v[V::kN];
-      V::unpack(u[k], v);
-      soft_add<ENT>(st, v, c);
+      for (int k = 0; k < kUnroll; ++k) {
+        float v[V::kN];
+        V::unpack(u[k], v);
+        soft_add<ENT>(st, v, c);
+      }
+    } else {  // what is left, its loads side by side too
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k)
+        if (i + k * NT < nv) u[k] = xv[i + k * NT];
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        if (i + k * NT >= nv) break;
+        float v[V::kN];
+        V::unpack(u[k], v);
+        soft_add<ENT>(st, v, c);
+      }
     }
-  }
-  for (; i < nv; i += NT) {
-    float v[V::kN];
-    V::unpack(xv[i], v);
-    soft_add<ENT>(st, v, c);
   }
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) {
@@ -204,12 +211,13 @@ __device__ __forceinline__ SoftStat row_stats(const T* x, int vocab, float c, So
     o.w = __shfl_xor(st.w, off);
     st = soft_join(st, o, c);
   }
-  if ((t & 63) == 0) part[t >> 6] = st;
-  __syncthreads();
-  st = part[0];
-#pragma unroll
-  for (int k = 1; k < NT / 64; ++k) st = soft_join(st, part[k], c);
-  __syncthreads();
+  if (NT > 64) {
+    if ((t & 63) == 0) part[t >> 6] = st;
+    __syncthreads();
+    st = part[0];
+    for (int k = 1; k < NT / 64; ++k) st = soft_join(st, part[k], c);
+    __syncthreads();
+  }
   return st;
 }
 
@@ -394,29 +402,28 @@ __global__ void __launch_bounds__(NT) logprob_bwd_kernel(const LogprobArgs a) {
         dv[i] = V::pack(y);
       };
       const T* xs = x + head;
-      int i = t;
       if (same) {
-        for (; i + (kUnroll - 1) * NT < nv; i += kUnroll * NT) {
+        for (int i = t; i < nv; i += kUnroll * NT) {
           uint4 u[kUnroll];
+          const bool whole = i - t + kUnroll * NT <= nv;
 #pragma unroll
-          for (int k = 0; k < kUnroll; ++k) u[k] = ((const uint4*)xs)[i + k * NT];
+          for (int k = 0; k < kUnroll; ++k)
+            if (whole || i + k * NT < nv) u[k] = ((const uint4*)xs)[i + k * NT];
 #pragma unroll
           for (int k = 0; k < kUnroll; ++k) {
+            if (!whole && i + k * NT >= nv) break;
             float v[V::kN];
             V::unpack(u[k], v);
             vec(i + k * NT, v);
           }
         }
-      }
-      for (; i < nv; i += NT) {
-        float v[V::kN];
-        if (same) {
-          V::unpack(((const uint4*)xs)[i], v);
-        } else {
+      } else {
+        for (int i = t; i < nv; i += NT) {
+          float v[V::kN];
 #pragma unroll
           for (int k = 0; k < V::kN; ++k) v[k] = (float)xs[i * V::kN + k];
+          vec(i, v);
         }
-        vec(i, v);
       }
     }
     __syncthreads();  // mark and the partial sums are reused by the next row
@@ -507,6 +514,11 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_small_kernel(const Poli
   __shared__ int bad, groups;
   const int t = threadIdx.x;
   constexpr int kPer = kPolicySmall / kPolicyThreads;
+  if (a.ng == 0) {  // nothing, and perhaps no arrays either
+    if (t < 4) a.stats[t] = 0.f;
+    if (t == 0) a.hdr->error = 0;
+    return;
+  }
   const int size = t < a.ng ? a.gsz[t] : 0;
   // the tokens are on their way while the grouping arrays are looked over
   float lp[kPer], old[kPer], ref[kPer];

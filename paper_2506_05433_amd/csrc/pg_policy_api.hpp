@@ -1,4 +1,4 @@
-// Entry points of the token log-probabilities and the policy loss (included by pg_attn.hip).
+// Entry points of the token log-probabilities and the policy loss (included by pg_lib.hip, after the helpers of pg_attn.hip).
 #pragma once
 
 namespace {
@@ -21,8 +21,9 @@ bool unaligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)
 
 template <typename T, int NT>
 void launch_logprobs(const pg::LogprobArgs& a, bool bwd, unsigned blocks, hipStream_t st) {
-  if (bwd) hipLaunchKernelGGL((pg::logprob_bwd_kernel<T, NT>), dim3(blocks), dim3(NT), 0, st, a);
-  else if (a.entropy) hipLaunchKernelGGL((pg::logprob_kernel<T, NT, true>), dim3(blocks), dim3(NT), 0, st, a);
+  if (bwd) {
+    if constexpr (NT > 64) hipLaunchKernelGGL((pg::logprob_bwd_kernel<T, NT>), dim3(blocks), dim3(NT), 0, st, a);
+  } else if (a.entropy) hipLaunchKernelGGL((pg::logprob_kernel<T, NT, true>), dim3(blocks), dim3(NT), 0, st, a);
   else hipLaunchKernelGGL((pg::logprob_kernel<T, NT, false>), dim3(blocks), dim3(NT), 0, st, a);
 }
 
@@ -43,10 +44,25 @@ int run_logprobs(int dtype, const pg::LogprobArgs& a0, bool bwd, const int32_t* 
     Timed tp_(PG_K_PLAN, st);
     if ((rc = launch_rope_plan(L, ws, a.ng, a.ns, tp, a.ts, a.cu_p, a.cu_s, gsz, st))) return rc;
   }
-  const unsigned blocks = (unsigned)std::min((long)a.ng + a.ts, 1L << 20);
+  // Threads a row, by its 16-byte pieces. 64: short rows where there are many, no barriers (5k rows, bf16: 1000 wide 8.8
+  // us against 15.9 with 256, 5000 wide 16.4 and 21.6, 17000 wide 36.2 and 35.4; as many waves as the card holds, each
+  // takes several rows). 1024: a few long rows (6 of 131072: 15.5, 17.9), and gradients of long rows, whose reads and
+  // writes then stay closer together (5k rows: 50001 wide bf16 203 us against 224, fp32 392 and 447; 17000 wide bf16
+  // 93 and 73).
+  const long rows = (long)a.ng + a.ts, pieces = a.vocab / (dtype == PG_BF16 ? 8 : 4);
+  const bool few = rows <= 128;
+  const bool wave = !bwd && pieces <= 1250 && rows >= 1024, long_rows = few ? pieces >= 2048 : bwd && pieces >= 4096;
+  const unsigned blocks = (unsigned)std::min(rows, wave ? 8192L : 1L << 20);
   Timed tm(PG_K_LOGPROBS, st);
-  if (dtype == PG_BF16) launch_logprobs<pg::bf16, 256>(a, bwd, blocks, st);
-  else launch_logprobs<float, 256>(a, bwd, blocks, st);
+  if (dtype == PG_BF16) {
+    if (wave) launch_logprobs<pg::bf16, 64>(a, bwd, blocks, st);
+    else if (long_rows) launch_logprobs<pg::bf16, 1024>(a, bwd, blocks, st);
+    else launch_logprobs<pg::bf16, 256>(a, bwd, blocks, st);
+  } else {
+    if (wave) launch_logprobs<float, 64>(a, bwd, blocks, st);
+    else if (long_rows) launch_logprobs<float, 1024>(a, bwd, blocks, st);
+    else launch_logprobs<float, 256>(a, bwd, blocks, st);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "token log-probability launch");
   return PG_OK;
@@ -162,7 +178,6 @@ int pg_policy_loss(int average, int n_groups, int n_suffixes, int total_suffix, 
   if (!workspace || workspace_bytes < L.total)
     return fail(PG_EWORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, L.total);
   if ((rc = device_ready())) return rc;
-  if (n_groups == 0) return PG_OK;
   hipStream_t st = (hipStream_t)stream;
   char* ws = (char*)workspace;
   pg::PolicyArgs a{};

@@ -271,3 +271,114 @@ def test_inconsistent_grouping_does_no_work():
             binding.plan_status(ws)
         assert e.value.status == 1
         assert all(bool((t == 3.0).all()) for t in out)
+
+
+SHORT = [  # few rows: no states between workgroups (P, members, h_q, h_kv, d, dtype)
+    (((64,), (4,), (24, 17, 0, 32)), 2, 2, 64, "fp32"),
+    (((60, 0, 68), (2, 1, 3), (10, 33, 7, 0, 5, 40)), 4, 4, 64, "bf16"),
+    (((100,), (2,), (20, 40)), 2, 1, 128, "bf16"),
+    (((33,), (5,), (1, 31, 32, 33, 2)), 4, 2, 128, "fp32"),
+    (((1, 3), (1, 1), (1, 200)), 1, 1, 128, "bf16"),
+]
+
+
+@pytest.mark.parametrize("case", range(len(SHORT)))
+def test_few_rows(case):
+    """The path without states between workgroups, against the oracle, and its initial states."""
+    from paper_2506_05433_amd import binding
+    lens, hq, hkv, d, dtype = SHORT[case]
+    prob = make_problem("tiny" if dtype == "fp32" else "single_group", seed=70 + case, lengths=lens, h_q=hq, h_kv=hkv, head_dim=d)
+    ld = _decays(hkv, case + 3)
+    print(f"[linear] few rows {SHORT[case]}", flush=True)
+    dev = binding.to_device(prob, "cuda")
+    grp = (dev["cu_prefix"], dev["cu_suffix"], dev["group_sizes"])
+    dld = torch.from_numpy(ld).cuda()
+    ref, mag = _oracles(prob, ld)
+    for n, x in zip(("o_pre", "o_suf"), binding.linear_fwd(*_args(dev), dld, *grp, prob.scale)):
+        _close(n, x, ref[n], mag[n], prob.dtype, _chain(prob))
+    for n, x in zip(GRADS, binding.linear_bwd(*_args(dev), dev["do_pre"], dev["do_suf"], dld, *grp, prob.scale)):
+        _close(n, x, ref[n], mag[n], prob.dtype, _chain(prob, 32))
+    s_in = np.random.default_rng(case).standard_normal((len(lens[0]), hkv, d, d)).astype(np.float32)
+    ref, mag = _oracles(prob, ld, state_in=s_in, grads=False)
+    for n, x in zip(("o_pre", "o_suf"), binding.linear_fwd(*_args(dev), dld, *grp, prob.scale, state_in=torch.from_numpy(s_in).cuda())):
+        _close(n, x, ref[n], mag[n], prob.dtype, _chain(prob) + 2)
+
+
+def _repeat_oracle_free(prob, ld, dev, grp, scale):
+    """The same problem with every member a group of its own prefix copy, by the library: forward and backward."""
+    from paper_2506_05433_amd import binding
+    pre, suf, at = [], [], 0
+    for p, size in zip(prob.prefix_lens, prob.group_sizes):
+        pre += [np.arange(at, at + p)] * int(size)
+        at += p
+    idx = torch.from_numpy(np.concatenate(pre)).cuda()
+    lens = np.repeat(prob.prefix_lens, prob.group_sizes)
+    i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    g2 = (i32(np.concatenate([[0], np.cumsum(lens)])), dev["cu_suffix"], i32(np.ones(len(lens))))
+    rep = lambda n: dev[n][idx].contiguous()  # noqa: E731
+    args = [rep("q_pre"), rep("k_pre"), rep("v_pre"), dev["q_suf"], dev["k_suf"], dev["v_suf"]]
+    o = binding.linear_fwd(*args, ld, *g2, scale)
+    share = torch.from_numpy(1.0 / np.repeat(np.repeat(prob.group_sizes, prob.group_sizes), lens)).cuda()
+    g = binding.linear_bwd(*args, (rep("do_pre").double() * share[:, None, None]).to(dev["do_pre"].dtype), dev["do_suf"], ld, *g2, scale)
+    summed = [torch.zeros(t.shape, dtype=torch.float64, device="cuda").index_add_(0, idx, x.double())
+              for t, x in zip((dev["q_pre"], dev["k_pre"], dev["v_pre"]), g[:3])]
+    return o, summed, g[3:]
+
+
+@pytest.mark.parametrize("lens,hq,hkv,d", [
+    (((900, 300), (40, 30), tuple(20 + 7 * i for i in range(70))), 16, 8, 64),     # whole members, ordered by length
+    (((257, 31, 0), (64, 4, 2), tuple([5, 260, 64, 0, 1, 33, 190] * 10)), 8, 8, 128),
+])
+def test_whole_members_equal_the_repeated_layout(lens, hq, hkv, d):
+    """Enough members that each is one item (longest first, states handed on by the gradient kernel): fp32, against the
+    library on the layout in which every member has its own copy of the prefix. Bound: both sides are within chain *
+    2^-23 of the magnitudes of the sums, which are at most 60 times the result's norm for these random rows."""
+    from paper_2506_05433_amd import binding
+    prob = make_problem("tiny", seed=91, lengths=lens, h_q=hq, h_kv=hkv, head_dim=d)
+    ld = torch.from_numpy(_decays(hkv, 3)).cuda()
+    print(f"[linear] whole members, {len(lens[2])} of them", flush=True)
+    dev = binding.to_device(prob, "cuda")
+    grp = (dev["cu_prefix"], dev["cu_suffix"], dev["group_sizes"])
+    o = binding.linear_fwd(*_args(dev), ld, *grp, prob.scale)
+    g = binding.linear_bwd(*_args(dev), dev["do_pre"], dev["do_suf"], ld, *grp, prob.scale)
+    ro, pre, suf = _repeat_oracle_free(prob, ld, dev, grp, prob.scale)
+    tol = 2 * 60 * 300 * 2.0 ** -23
+    for name, a, b in [("o_suf", o[1], ro[1])] + list(zip(GRADS, g, list(pre) + list(suf))):
+        err = float((a.double() - b.double()).norm() / b.double().norm())
+        print(f"  {name}: {err:.2e}", flush=True)
+        assert err <= tol, (name, err)
+
+
+def test_both_planners_agree(monkeypatch):
+    """The items of the planner for large grouping arrays, forced, give the same bits."""
+    from paper_2506_05433_amd import binding
+    prob = make_problem("single_group", seed=92, lengths=((300, 90), (40, 31), tuple(10 + 3 * i for i in range(71))), h_q=16,
+                        h_kv=8, head_dim=64)
+    ld = torch.from_numpy(_decays(8, 3)).cuda()
+    dev = binding.to_device(prob, "cuda")
+    grp = (dev["cu_prefix"], dev["cu_suffix"], dev["group_sizes"])
+
+    def both():
+        o = binding.linear_fwd(*_args(dev), ld, *grp, prob.scale, states=True)
+        return o + binding.linear_bwd(*_args(dev), dev["do_pre"], dev["do_suf"], ld, *grp, prob.scale)
+
+    one = both()
+    monkeypatch.setenv("PG_PLAN_MULTI", "1")
+    for a, b in zip(one, both()):
+        assert torch.equal(a, b)
+
+
+def test_a_stray_value_stays_in_its_member():
+    """NaN in one member's rows reaches neither the prefix's and the other members' outputs nor, without it in the upstream
+    gradient, their own rows' gradients of q."""
+    from paper_2506_05433_amd import binding
+    prob = make_problem("single_group", seed=93, lengths=((70, 10), (3, 1), (40, 33, 70, 9)), h_q=4, h_kv=2, head_dim=128)
+    ld = torch.from_numpy(_decays(2, 3)).cuda()
+    dev = binding.to_device(prob, "cuda")
+    grp = (dev["cu_prefix"], dev["cu_suffix"], dev["group_sizes"])
+    clean = binding.linear_fwd(*_args(dev), ld, *grp, prob.scale)
+    dev["v_suf"][45] = float("nan")  # the second member
+    o = binding.linear_fwd(*_args(dev), ld, *grp, prob.scale)
+    keep = torch.cat([torch.arange(0, 40), torch.arange(73, prob.total_suffix)]).cuda()
+    assert torch.equal(o[0], clean[0]) and torch.equal(o[1][keep], clean[1][keep])
+    assert bool(torch.isnan(o[1][45:73]).any(-1).all())

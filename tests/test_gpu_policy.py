@@ -311,3 +311,63 @@ def test_captured_with_eager_work_between():
         torch.cuda.synchronize()
         for i, (a, b) in enumerate(zip(outs, eager)):
             assert torch.equal(a, b), f"replay {rep}, output {i}"
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("lens,vocab", [(((5, 3), (9, 40), tuple([30] * 9 + [25] * 40)), 301),
+                                        (((2,), (700,), tuple([13] * 700)), 40)])
+def test_many_short_rows(lens, vocab, dt):
+    """Many rows of few elements, whole groups' first tokens among them: every row against float64, and the gradient."""
+    from paper_2506_05433_amd import binding
+    ts, ng = sum(lens[2]), len(lens[0])
+    print(f"[logprobs] {ts} rows of {vocab} {dt}", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    last, suf = (torch.randn(n, vocab, generator=gen, device="cuda").mul_(2).to(dt) for n in (ng, ts))
+    tok = torch.randint(0, vocab, (ts,), generator=gen, device="cuda")
+    d = torch.randn(ts, generator=gen, device="cuda")
+    lp, lse, ent = binding.token_logprobs(last, suf, tok, *_grp(lens), sum(lens[0]), entropy=True)
+    cu = np.concatenate([[0], np.cumsum(lens[2])])
+    group = np.repeat(np.repeat(np.arange(ng), lens[1]), lens[2])
+    first = np.isin(np.arange(ts), cu[:-1])
+    src = torch.from_numpy(np.where(first, ng * 0 + group, ng + np.arange(ts) - 1)).cuda()
+    x = torch.cat([last, suf]).double()[src]
+    ref = torch.log_softmax(x, 1)
+    zmax = float(x.abs().max())
+    tol = 2.0 ** -22 * (zmax + vocab / 64 + 40)   # one wave a row: vocab / 64 additions in a row at most
+    assert float((lp.double() - ref.gather(1, tok[:, None])[:, 0]).abs().max()) <= tol
+    assert float((lse.double() - torch.logsumexp(x, 1)).abs().max()) <= tol
+    assert float((ent.double() + (ref.exp() * ref).sum(1)).abs().max()) <= tol * (1 + 2 * zmax)
+    gl, gs = binding.token_logprobs_bwd(last, suf, tok, lse, d, *_grp(lens), sum(lens[0]))
+    g = -ref.exp() * d.double()[:, None]
+    g[torch.arange(ts, device="cuda"), tok] += d.double()
+    want = torch.zeros(ng + ts, vocab, dtype=torch.float64, device="cuda").index_add_(0, src, g)
+    w = torch.zeros(ng + ts, dtype=torch.float64, device="cuda").index_add_(0, src, d.double().abs())
+    lim = U[dt] * want.abs() * 1.01 + (2.0 ** -23 * (2 * zmax + 8) + tol + max(lens[1]) * 2.0 ** -23) * w[:, None]
+    assert bool(((torch.cat([gl, gs]).double() - want).abs() <= lim).all())
+
+
+def test_long_batches_without_a_mask_and_many_members():
+    """The paths for more tokens than one workgroup takes, without a mask; and for more members than fit LDS."""
+    from paper_2506_05433_amd import binding
+    for lens, average in ((((1, 1), (3, 2), (5000, 0, 7001, 300, 40)), "group"), (((1, 1), (3, 2), (5000, 0, 7001, 300, 40)), "token"),
+                          (((1,), (4200,), tuple(i % 3 for i in range(4200))), "group")):
+        ts, ns = sum(lens[2]), len(lens[2])
+        print(f"[policy] {ns} members, {ts} tokens, {average}", flush=True)
+        rng = np.random.default_rng(ts)
+        lp = -rng.uniform(0, 5, ts).astype(np.float32)
+        old, adv = (lp + 0.3 * rng.standard_normal(ts)).astype(np.float32), rng.standard_normal(ns).astype(np.float32)
+        want, grad = policy_loss_oracle(lens[1], lens[2], lp, adv, old, average=average)
+        _, cs, gs = _grp(lens)
+        t = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+        stats, d = binding.policy_loss(t(lp), t(adv), cs, gs, logp_old=t(old), average=average)
+        assert (np.abs(stats.double().cpu().numpy() - want) <= 2.0 ** -24 * np.abs(want) + 1e-12 * (1 + np.abs(want).sum())).all()
+        assert (np.abs(d.double().cpu().numpy() - grad) <= 2.0 ** -24 * np.abs(grad) + 1e-14).all()
+
+
+def test_policy_loss_of_no_groups_is_zero():
+    from paper_2506_05433_amd import binding
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    none = torch.empty(0, device="cuda")
+    out = (torch.full((4,), 3.0, device="cuda"), none)
+    binding.policy_loss(none, none, i32([0]), i32([]), out=out)
+    assert bool((out[0] == 0).all())
