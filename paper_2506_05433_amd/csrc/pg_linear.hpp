@@ -9,7 +9,8 @@
 // *item*, at most L rows of one segment (a prefix or a member), and keeps a copy of it in the tensors' type in LDS as
 // an operand. Items run side by side, so the states between them come first: state kernel (each item's own share),
 // scan kernels (prefixes, then members, in item order), then the kernel that writes the outputs. A member of one item
-// needs no share: it starts from the prefix's state.
+// needs no share: it starts from the prefix's state. All of it is bound by memory (a row of a query head is 4 D
+// elements read and written for 4 D^2 multiply-adds and its share of a state update), small calls by launches.
 //
 // Gradients: dq is the same walk with do in the place of q, v of k and k of v. dk and dv walk each segment backwards
 // with R_s = l R_{s+1} + sum_heads q_s do_s^T, members first; a prefix starts from the sum of its members' states, in
@@ -83,13 +84,24 @@ __device__ __forceinline__ int item_place(int r, int n, int round) {
 __device__ __forceinline__ void lin_items(const LinList& L, const int* cu_p, const int* cu_s, const GroupInfoEx* ginfo,
                                           int ng, int ns, int* off, int* tmp, int& carry, int* work) {
   const int t = threadIdx.x, segs = ng + ns;
+  auto count = [&](int s) {
+    if (s >= segs) return 0;
+    return s < ng ? ceil_div(cu_p[s + 1] - cu_p[s], L.l_pre) : ceil_div(cu_s[s - ng + 1] - cu_s[s - ng], L.l_suf);
+  };
   __syncthreads();
   if (t == 0) carry = 0;
   __syncthreads();
-  for (int base = 0; base < segs; base += kPlanThreads) {
+  if (segs < kPlanThreads) {  // one segment a thread: wave scans, two barriers
+    int n[1] = {count(t)};
+    block_exclusive_sums(n, segs, (int(*)[kPlanThreads / 64])tmp);
+    if (t <= segs) off[t] = n[0];
+    if (t < segs && off != L.seg_off) L.seg_off[t] = n[0];
+    if (t == segs) carry = n[0];
+    __syncthreads();
+  }
+  for (int base = segs < kPlanThreads ? segs : 0; base < segs; base += kPlanThreads) {
     const int s = base + t;
-    int n = 0;
-    if (s < segs) n = s < ng ? ceil_div(cu_p[s + 1] - cu_p[s], L.l_pre) : ceil_div(cu_s[s - ng + 1] - cu_s[s - ng], L.l_suf);
+    const int n = count(s);
     const int inc = block_inclusive_scan<kPlanThreads>(n, tmp);
     if (s < segs) {
       off[s] = carry + inc - n;
@@ -148,7 +160,7 @@ __global__ void __launch_bounds__(kPlanThreads) lin_items_kernel(const int* __re
                                                                  const int* __restrict__ cu_s, int ng, int ns,
                                                                  const LinList L, const PlanHeader* hdr,
                                                                  const GroupInfoEx* __restrict__ ginfo) {
-  __shared__ int tmp[kPlanThreads];
+  alignas(16) __shared__ int tmp[kPlanThreads];
   __shared__ int carry;
   if (hdr->error) {
     if (threadIdx.x == 0) *L.n_items = 0;
@@ -167,6 +179,7 @@ __global__ void __launch_bounds__(kPlanThreads) lin_plan_kernel(const int* __res
                                                                 int lists) {
   __shared__ PlanLds lds;
   __shared__ int off[kLdsGroups + kLdsMembers + 1];
+  alignas(16) __shared__ int tmp[kPlanThreads];
   __shared__ int carry;
   const bool ok = plan_groups_lds(cu_p, cu_s, gsz, ng, ns, tp, ts, kFwdBM, kKvBN, 1, 0, 0x7fffffffL, 0x7fffffffL, hdr,
                                   ginfo, qoff, kvoff, lds);
@@ -178,12 +191,14 @@ __global__ void __launch_bounds__(kPlanThreads) lin_plan_kernel(const int* __res
     }
     return;
   }
-  lin_items(a, lds.cu_p, lds.cu_s, lds.gi, ng, ns, off, lds.part, carry, lds.work[0]);
-  if (lists > 1) lin_items(b, lds.cu_p, lds.cu_s, lds.gi, ng, ns, off, lds.part, carry, lds.work[1]);
+  lin_items(a, lds.cu_p, lds.cu_s, lds.gi, ng, ns, off, tmp, carry, lds.work[0]);
+  if (lists > 1) lin_items(b, lds.cu_p, lds.cu_s, lds.gi, ng, ns, off, tmp, carry, lds.work[1]);
 }
 
 // ---------------------------------------------------------------- pieces of the walks
-// Tile shapes of a walk: C rows a chunk, NW waves.
+// Tile shapes of a walk: C rows a chunk, NW waves. 32 rows of 128-wide bf16 heads leave room for two workgroups on a CU
+// (80 KB each), which hide one another's loads and barriers; 128-row chunks with one workgroup of eight waves have half
+// the vector work a row and ran no faster (932 us against 899).
 template <typename T, int D, int C, int NW>
 struct LinTiles {
   static constexpr int kC = C, kNW = NW, kNT = 64 * NW;
@@ -379,9 +394,10 @@ __device__ __forceinline__ void rows_to_lds(const f32x16 (&acc)[N], char* tile, 
 }
 
 // The first `valid` rows of an LDS tile to memory, by the mapping of the loader that brings in such tiles: 16 bytes a
-// lane, whole rows by consecutive lanes (stores straight from the accumulators are 16-byte pieces of 32 rows each, and
-// cost the cache as much as full lines: 1270 -> 700 us without them where the outputs of 78k rows x 40 heads took 1270).
-// Rows past the range are dropped, without a branch: a wait for a later load would otherwise wait for the stores too.
+// lane, whole rows by consecutive lanes. Stores straight from the accumulators are 16-byte pieces of 32 rows, loads
+// straight into operands 32-byte ones, and the cache takes as long for each as for a line: the output kernel of 78k rows
+// x 40 heads ran 1270 us with both, 580 through LDS. Rows past the range are dropped, without a branch: a wait for a
+// later load would otherwise wait for the stores too.
 template <typename T, int ROWS, int D, int NT>
 __device__ __forceinline__ void tile_to_memory(const TileLoader<T, ROWS, D, NT>& m, const char* tile, T* base,
                                                int gstride, int valid) {
@@ -485,7 +501,6 @@ __global__ void __launch_bounds__(kScanThreads) lin_scan_kernel(const LinArgs a)
   using S = ScanVec<PART>;
   using V = typename S::type;
   constexpr int kBatch = S::kBatch;
-  if (a.hdr->error) return;
   const int kv = blockIdx.y;
   const size_t e = S::kN * ((size_t)blockIdx.x * kScanThreads + threadIdx.x), per = (size_t)D * D;
   const float g = log2_decay(a.log_decay, kv);
@@ -498,6 +513,7 @@ __global__ void __launch_bounds__(kScanThreads) lin_scan_kernel(const LinArgs a)
     // the last item holds what the others leave
     const int len = PART ? a.cu_s[seg + 1] - a.cu_s[seg] : a.cu_p[seg + 1] - a.cu_p[seg];
     const float tail = fast_exp2(g * (float)(len - max(i1 - i0 - 1, 0) * (PART ? a.l_suf : a.l_pre)));
+    if (a.hdr->error) return;  // loaded beside the offsets, which mean nothing then
     V st = {};
     if (!PART) {
       if (REV) {  // the members' states, in member order

@@ -59,9 +59,9 @@ ItemRows linear_item_rows(int ns, int tp, int ts, int h_q, int h_kv, int d, bool
   // 1024 rows: forward state and output 29 + 111, 27 + 110, 38 + 187 us, backward 99 + 152, 81 + 157, 112 + 257;
   // P 4096, 128, 256 and 512: 19 + 52, 16 + 49, 21 + 78; P 400 of 2, a whole backward with 32, 64, 128 and 256: 47, 55,
   // 77 and 123
-  const long groups = many ? (long)ns * heads : ts / r.suf * heads;
+  const long groups = many ? (long)ns * heads : (long)ts / r.suf * heads;
   r.pre = 1024;
-  while (r.pre > least && ((long)tp * h_kv < (grad ? 256L : 128L) * r.pre || tp / r.pre * heads + groups < 400)) r.pre /= 2;
+  while (r.pre > least && ((long)tp * h_kv < (grad ? 256L : 128L) * r.pre || (long)tp / r.pre * heads + groups < 400)) r.pre /= 2;
   r.members_first = many;
   r.round = many ? (int)ceil_div_l(256, heads) : 0;
   return r;
