@@ -44,6 +44,7 @@ int run_logprobs(int dtype, const pg::LogprobArgs& a0, bool bwd, const int32_t* 
     Timed tp_(PG_K_PLAN, st);
     if ((rc = launch_rope_plan(L, ws, a.ng, a.ns, tp, a.ts, a.cu_p, a.cu_s, gsz, st))) return rc;
   }
+  if (!bwd && a.ts == 0) return PG_OK;  // no token to predict: no logits are read, they may be NULL
   // Threads a row, by its 16-byte pieces. 64: short rows where there are many, no barriers (5k rows, bf16: 1000 wide 8.8
   // us against 15.9 with 256, 5000 wide 16.4 and 21.6, 17000 wide 36.2 and 35.4; as many waves as the card holds, each
   // takes several rows). 1024: a few long rows (6 of 131072: 15.5, 17.9), and gradients of long rows, whose reads and

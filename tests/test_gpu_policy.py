@@ -371,3 +371,21 @@ def test_policy_loss_of_no_groups_is_zero():
     out = (torch.full((4,), 3.0, device="cuda"), none)
     binding.policy_loss(none, none, i32([0]), i32([]), out=out)
     assert bool((out[0] == 0).all())
+
+
+def test_no_response_rows():
+    """Members without a row: nothing to predict, logits are not read (they may be NULL); the gradient is zeros."""
+    from paper_2506_05433_amd import binding
+    cp, cs, gs = _grp(((3, 0), (2, 1), (0, 0, 0)))
+    ws = torch.empty(binding.token_logprobs_workspace_bytes(2, 3, 0, 50), dtype=torch.uint8, device="cuda")
+    p = lambda t: t.data_ptr()  # noqa: E731
+    st = binding.lib().pg_token_logprobs(1, 8, 2, 3, 3, 0, p(cp), p(cs), p(gs), 50, 1.0, None, 50, None, 50, None, None, None,
+                                         None, p(ws), ws.numel(), torch.cuda.current_stream().cuda_stream)
+    assert st == 0, binding.lib().pg_last_error()
+    torch.cuda.synchronize()
+    none = torch.empty(0, device="cuda")
+    last = torch.full((2, 50), float("nan"), device="cuda")
+    out = binding.token_logprobs(last, none.view(0, 50), none.long(), cp, cs, gs, 3, entropy=True)
+    assert [t.numel() for t in out] == [0, 0, 0]
+    gl, _ = binding.token_logprobs_bwd(last, none.view(0, 50), none.long(), none, none, cp, cs, gs, 3)
+    assert bool((gl == 0).all())
