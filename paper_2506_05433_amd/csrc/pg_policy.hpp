@@ -245,7 +245,8 @@ __global__ void __launch_bounds__(NT) logprob_kernel(const LogprobArgs a) {
     const T* x = row.group >= 0 ? (const T*)a.last + row.group * a.ld_last : (const T*)a.suf + (b - a.ng) * a.ld_suf;
     const SoftStat st = row_stats<T, NT, ENT>(x, a.vocab, c, part);
     // ln sum exp(x / T), and the entropy ln s - sum p ln 2 c (x - m)
-    const bool none = st.m == -INFINITY;
+    // (a maximum passes over NaN, the sum does not: a row of NaN and -inf has s = NaN, one of -inf alone s = 0)
+    const bool none = st.m == -INFINITY && st.s == 0.f;
     const float ln_s = logf(st.s);
     const float lse = none ? -INFINITY : st.m * a.inv_temp + ln_s;
     float ent = none ? 0.f : ln_s - kLn2 * st.w / st.s;

@@ -389,3 +389,20 @@ def test_no_response_rows():
     assert [t.numel() for t in out] == [0, 0, 0]
     gl, _ = binding.token_logprobs_bwd(last, none.view(0, 50), none.long(), none, none, cp, cs, gs, 3)
     assert bool((gl == 0).all())
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("vocab", [1, 13, 3000])
+def test_rows_of_nothing_but_nan(dt, vocab):
+    """A row of NaN, and one of NaN and -inf, is NaN throughout, not a row with nothing left; so is its gradient."""
+    from paper_2506_05433_amd import binding
+    last = torch.full((1, vocab), float("nan"), dtype=dt, device="cuda")
+    suf = torch.zeros(4, vocab, dtype=dt, device="cuda")
+    suf[0], suf[1], suf[1, vocab // 2] = float("nan"), -float("inf"), float("nan")
+    tok, g = torch.zeros(4, dtype=torch.int64, device="cuda"), _grp(((2,), (1,), (4,)))
+    lp, lse, ent = binding.token_logprobs(last, suf, tok, *g, 2, entropy=True)
+    for t in (lp, lse, ent):
+        assert t.isnan().tolist() == [True, True, True, False]
+    gl, gs = binding.token_logprobs_bwd(last, suf, tok, lse, torch.ones(4, device="cuda"), *g, 2)
+    assert bool(gl.isnan().all()) and gs.isnan().all(1).tolist() == [True, True, False, False]
+    assert not bool(gs[2:].isnan().any())
