@@ -313,7 +313,8 @@ int pg_linear_step(int dtype, int n, int h_q, int h_kv, int head_dim, float scal
  *   logp[r] = x[token] - lse[r],  lse[r] = ln sum exp x,  entropy[r] = -sum p ln p   (float [total_suffix]).
  * entropy may be NULL (it is for monitoring and has no gradient). A token outside [0, vocab) (padding) gets logp 0
  * and no gradient. Logits of -inf are legal; a row of nothing else gives logp = lse = -inf, entropy 0 and a zero
- * gradient. Where a prefix is empty nothing predicts its members' first tokens: logp 0, lse -inf, entropy 0, and that
+ * gradient. (lse out of fp32's range below, a row masked with the type's lowest value at temperature < 1, is stored as
+ * the lowest finite value.) Where a prefix is empty nothing predicts its members' first tokens: logp 0, lse -inf, entropy 0, and that
  * row of logits_last is not read.
  *
  * The gradient: dlogits = (1 / temperature) sum over the row's targets of dlogp (onehot - softmax), with lse as the

@@ -9,6 +9,7 @@
 // log-sum-exp. Rows start at any alignment the element type has; a row's first elements up to a 16-byte boundary and
 // its last ones are taken one by one.
 #pragma once
+#include <cfloat>
 #include "pg_common.hpp"
 #include "pg_plan.hpp"
 
@@ -248,7 +249,8 @@ __global__ void __launch_bounds__(NT) logprob_kernel(const LogprobArgs a) {
     // (a maximum passes over NaN, the sum does not: a row of NaN and -inf has s = NaN, one of -inf alone s = 0)
     const bool none = st.m == -INFINITY && st.s == 0.f;
     const float ln_s = logf(st.s);
-    const float lse = none ? -INFINITY : st.m * a.inv_temp + ln_s;
+    float lse = none ? -INFINITY : st.m * a.inv_temp + ln_s;
+    if (lse == -INFINITY && !none) lse = -FLT_MAX;  // m / T is out of range: -inf is for rows with nothing left
     float ent = none ? 0.f : ln_s - kLn2 * st.w / st.s;
     if (ent < 0.f) ent = 0.f;  // by rounding only; a NaN stays
     auto put = [&](int r) {

@@ -406,3 +406,23 @@ def test_rows_of_nothing_but_nan(dt, vocab):
     gl, gs = binding.token_logprobs_bwd(last, suf, tok, lse, torch.ones(4, device="cuda"), *g, 2)
     assert bool(gl.isnan().all()) and gs.isnan().all(1).tolist() == [True, True, False, False]
     assert not bool(gs[2:].isnan().any())
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+def test_rows_of_the_lowest_value_divided_by_a_temperature(dt):
+    """The log-sum-exp of such a row is out of fp32's range; its log-probabilities and gradient are a uniform row's."""
+    from paper_2506_05433_amd import binding
+    vocab, temp = 13, 0.5
+    suf = torch.zeros(2, vocab, dtype=dt, device="cuda")
+    suf[0] = torch.finfo(dt).min
+    tok, g = torch.tensor([0, 4], device="cuda"), _grp(((0,), (1,), (2,)))
+    last = torch.zeros(1, vocab, dtype=dt, device="cuda")
+    lp, lse = binding.token_logprobs(last, suf, tok, *g, 0, temperature=temp)
+    # ln 13 < 4 by 13 terms of 1: its rounding and the function's, 2^-21 at most
+    assert abs(lp[1].item() + np.log(vocab)) <= 2.0 ** -20 and lse[1].item() == torch.finfo(torch.float32).min
+    _, gs = binding.token_logprobs_bwd(last, suf, tok, lse, torch.ones(2, device="cuda"), *g, 0, temperature=temp)
+    want = np.full(vocab, -1.0 / vocab)
+    want[4] += 1.0
+    u = U[dt] + 2.0 ** -21  # the result's rounding; w, p and the target's sum, three of fp32
+    assert (np.abs(gs[0].double().cpu().numpy() - want / temp) <= u * np.abs(want) / temp).all()
+    assert bool((gs[1] == 0).all())
