@@ -226,6 +226,10 @@ bool misaligned(std::initializer_list<const void*> ps) {
   return false;
 }
 
+bool overlap(const void* p, const void* q, size_t p_bytes, size_t q_bytes) {
+  return p && q && (uintptr_t)p < (uintptr_t)q + q_bytes && (uintptr_t)q < (uintptr_t)p + p_bytes;
+}
+
 }  // namespace
 
 extern "C" {
@@ -259,6 +263,9 @@ int pg_linear_fwd(int dtype, int n_groups, int n_suffixes, int total_prefix, int
   if (total_suffix > 0 && (!q_suf || !k_suf || !v_suf || !o_suf)) return fail(PG_EINVAL, "a suffix tensor pointer is NULL");
   if (misaligned({q_pre, k_pre, v_pre, q_suf, k_suf, v_suf, state_in, o_pre, o_suf, state_pre, state_suf, workspace}))
     return fail(PG_EINVAL, "tensor pointers must be 16-byte aligned");
+  const size_t state = sizeof(float) * (size_t)h_kv * head_dim * head_dim, in = state * n_groups;
+  if (overlap(state_in, state_pre, in, in) || overlap(state_in, state_suf, in, state * n_suffixes))
+    return fail(PG_EINVAL, "state_in overlaps state_pre or state_suf");
   const LinearLayout L = linear_layout(state_pre || state_suf ? -1 : dtype, c.ng, c.ns, c.tp, c.ts, c.h_q, c.h_kv, c.d, false);
   if ((rc = linear_grid_check(c, L.out))) return rc;
   if (!workspace || workspace_bytes < L.total)
@@ -347,6 +354,9 @@ int pg_linear_step(int dtype, int n, int h_q, int h_kv, int head_dim, float scal
   if (!log_decay || (n > 0 && (!q || !k || !v || !state || !o || !state_out)))
     return fail(PG_EINVAL, "a tensor pointer is NULL");
   if (misaligned({q, k, v, state, o, state_out})) return fail(PG_EINVAL, "tensor pointers must be 16-byte aligned");
+  const size_t states_bytes = sizeof(float) * (size_t)n * h_kv * head_dim * head_dim;
+  if (state_out != state && overlap(state, state_out, states_bytes, states_bytes))
+    return fail(PG_EINVAL, "state_out overlaps state without being state");
   int rc = device_ready();
   if (rc || n == 0) return rc;
   pg::LinStepArgs a{q, k, v, log_decay, state, o, state_out, n, h_q, h_kv, scale};

@@ -149,3 +149,17 @@ def test_binding_refuses_host_and_misshapen_tensors():
         binding.policy_loss(_t(6), _t(2), *grp[1:], average="mean")
     with pytest.raises(ValueError, match="advantages has shape"):
         binding.policy_loss(_t(6), _t(3), *grp[1:])
+
+
+def test_linear_states_must_not_overlap():
+    """A state read while it is written: the prefixes' states written over the ones they start from, and single tokens' states
+    shifted against themselves."""
+    assert _linear("fwd", state_in=1 << 20, states=1 << 20) == EINVAL and b"overlaps" in binding.lib().pg_last_error()
+    assert _linear("fwd", state_in=1 << 20, states=(1 << 20) + 64) == EINVAL and b"overlaps" in binding.lib().pg_last_error()
+    # 1 group of 2 heads, 2 members: 128 KiB and 256 KiB
+    assert _linear("fwd", state_in=(1 << 20) + (128 << 10), states=1 << 20) == EINVAL
+    assert _linear("fwd", state_in=(1 << 20) + (256 << 10), states=1 << 20, ws=0) == EWORKSPACE
+    assert _linear("fwd", state_in=1 << 20, states=(1 << 20) + (128 << 10), ws=0) == EWORKSPACE
+    step = lambda out: binding.lib().pg_linear_step(0, 3, 4, 2, 64, 1.0, *[P(64)] * 4, P(1 << 20), P(64), P(out), None)  # noqa: E731
+    assert step((1 << 20) + 16) == EINVAL and b"overlaps" in binding.lib().pg_last_error()
+    assert step((1 << 20) - 96 * 1024 + 16) == EINVAL
