@@ -23,6 +23,7 @@ struct LogprobArgs {
   int tok64;
   float *logp, *lse, *entropy;
   const float* dlogp;
+  float* target;  // [n_suffixes]: gradient at the first token of each member, summed over those that share it
   const int *cu_p, *cu_s;
   const PlanHeader* hdr;
   const GroupInfoEx* ginfo;
@@ -272,15 +273,18 @@ __global__ void __launch_bounds__(NT) logprob_kernel(const LogprobArgs a) {
 
 // dlogits = (1 / T) sum over the row's targets of dlogp (onehot - softmax). A row without a target, or whose targets
 // all have dlogp = 0 or a token outside the vocabulary, or with no finite logit, gets zeros and is not read.
-// A group row marks its targets' 16-byte pieces in an LDS bitmap (a hash: false hits only cost time) and, where a
-// piece is marked, walks the members in order.
-constexpr int kMarkBits = 8192;
+// The row that a group's members share has many targets. One thread a member sums what the members with its token add,
+// in member order, and forms that element's gradient before the row is written (it may be written over the logits); the
+// row is written as if it had no target, and the targets' elements after it. (One group, two rows a member, 32000 wide:
+// 64, 256 and 1024 members 159, 811 and 3226 us when every 16 bytes with a target walked the members, 17, 20 and 74 now.)
+constexpr int kStaged = 1024;  // members in LDS at a time
 
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT) logprob_bwd_kernel(const LogprobArgs a) {
   using V = Vec16<T>;
   constexpr int kUnroll = 4;
-  __shared__ unsigned mark[kMarkBits / 32];
+  alignas(16) __shared__ int staged_tok[kStaged];  // first tokens of the group's members, -1 where there is no gradient
+  alignas(16) __shared__ float staged_d[kStaged];
   __shared__ float sum_part[NT / 64], lse_part[NT / 64];
   __shared__ int any_part[NT / 64];
   __shared__ SoftStat stat_part[NT / 64];
@@ -297,23 +301,24 @@ __global__ void __launch_bounds__(NT) logprob_bwd_kernel(const LogprobArgs a) {
     const bool same = (((uintptr_t)x ^ (uintptr_t)dx) & 15) == 0;
     float total = 0.f, lse = -INFINITY, d1 = 0.f;
     int tok1 = -1, any = 0;
+    // the token that member m starts with and its gradient; false where there is none
+    auto first_token = [&](int m, int& tok, float& d) {
+      const int r = a.cu_s[m];
+      if (r == a.cu_s[m + 1]) return false;
+      tok = token_at(a, r);
+      d = a.dlogp[r];
+      return tok >= 0 && d != 0.f;
+    };
     if (grp) {
-      for (int i = t; i < kMarkBits / 32; i += NT) mark[i] = 0;
-      __syncthreads();
       float sum = 0.f, l = -INFINITY;
       for (int m = row.m0 + t; m < row.m1; m += NT) {
         const int r = a.cu_s[m];
-        if (r == a.cu_s[m + 1]) continue;
-        const int tok = token_at(a, r);
-        l = a.lse[r];  // the same for every member: the row's own
-        const float d = a.dlogp[r];
-        if (tok < 0 || d == 0.f) continue;
+        if (r < a.cu_s[m + 1]) l = a.lse[r];  // the same for every member: the row's own
+        int tok;
+        float d;
+        if (!first_token(m, tok, d)) continue;
         any = 1;
         sum += d;
-        if (tok >= head && tok < tail) {
-          const int p = ((tok - head) / V::kN) % kMarkBits;
-          atomicOr(&mark[p / 32], 1u << (p % 32));
-        }
       }
       // a fixed order: the members of a lane, the lanes of a wave, the waves
 #pragma unroll
@@ -347,15 +352,6 @@ __global__ void __launch_bounds__(NT) logprob_bwd_kernel(const LogprobArgs a) {
         tok1 = -1;
       }
     }
-    // what a member whose first token is `tok` adds: the members in order
-    auto hits = [&](int e0, int n, float* add) {
-      for (int m = row.m0; m < row.m1; ++m) {
-        const int r = a.cu_s[m];
-        if (r == a.cu_s[m + 1]) continue;
-        const int tok = token_at(a, r);
-        if (tok >= e0 && tok < e0 + n) add[tok - e0] += a.dlogp[r];
-      }
-    };
     if (lse == -INFINITY) any = 0;
     // p = 2^(c x - lse log2 e); where the log-sum-exp is too large for that it has also lost ln s (a row masked with
     // the type's lowest value throughout), and the statistics are taken again: p = 2^(c (x - m)) / s
@@ -368,14 +364,43 @@ __global__ void __launch_bounds__(NT) logprob_bwd_kernel(const LogprobArgs a) {
       w /= st.s;
     }
     auto prob = [&](float v) { return fast_exp2(far ? c * (v - top) : fmaf(c, v, off)); };
+    if (grp && any) {
+      const int n = row.m1 - row.m0;
+      for (int i0 = 0; i0 < n; i0 += NT) {
+        int mine = -1;
+        float d, add = 0.f;
+        if (i0 + t < n && !first_token(row.m0 + i0 + t, mine, d)) mine = -1;
+        for (int j0 = 0; j0 < n; j0 += kStaged) {
+          const int here = min(kStaged, n - j0), up = (here + 3) & ~3;
+          if (i0 == 0 || n > kStaged) {
+            __syncthreads();
+            for (int j = t; j < up; j += NT) {
+              int tok = -1;
+              float dj = 0.f;
+              const bool has = j < here && first_token(row.m0 + j0 + j, tok, dj);
+              staged_tok[j] = has ? tok : -1;
+              staged_d[j] = dj;
+            }
+            __syncthreads();
+          }
+          if (mine >= 0)
+#pragma unroll 4
+            for (int j = 0; j < up; j += 4) {
+              const int4 q = *(const int4*)(staged_tok + j);
+              const f32x4 v = *(const f32x4*)(staged_d + j);
+              add += q.x == mine ? v[0] : 0.f;
+              add += q.y == mine ? v[1] : 0.f;
+              add += q.z == mine ? v[2] : 0.f;
+              add += q.w == mine ? v[3] : 0.f;
+            }
+        }
+        if (mine >= 0) a.target[row.m0 + i0 + t] = fmaf(add, a.inv_temp, prob((float)x[mine]) * w);
+      }
+      __syncthreads();  // the targets' logits have been read
+    }
     auto one = [&](int e) {
       float y = 0.f;
-      if (any) {
-        float add = 0.f;
-        if (grp) hits(e, 1, &add);
-        else if (e == tok1) add = d1;
-        y = fmaf(add, a.inv_temp, prob((float)x[e]) * w);  // as vec() forms it, bit for bit
-      }
+      if (any) y = fmaf(e == tok1 ? d1 : 0.f, a.inv_temp, prob((float)x[e]) * w);  // as vec() forms it, bit for bit
       dx[e] = (T)y;
     };
     if (t < head) one(t);
@@ -389,15 +414,7 @@ __global__ void __launch_bounds__(NT) logprob_bwd_kernel(const LogprobArgs a) {
 #pragma unroll
         for (int k = 0; k < V::kN; ++k) y[k] = prob(v[k]) * w;
         const int e0 = head + i * V::kN;
-        if (grp) {
-          const int p = i % kMarkBits;
-          if (mark[p / 32] >> (p % 32) & 1) {
-            float add[V::kN] = {};
-            hits(e0, V::kN, add);
-#pragma unroll
-            for (int k = 0; k < V::kN; ++k) y[k] = fmaf(add[k], a.inv_temp, y[k]);
-          }
-        } else if ((unsigned)(tok1 - e0) < (unsigned)V::kN) {
+        if ((unsigned)(tok1 - e0) < (unsigned)V::kN) {
 #pragma unroll
           for (int k = 0; k < V::kN; ++k)
             if (tok1 - e0 == k) y[k] = fmaf(d1, a.inv_temp, y[k]);
@@ -429,7 +446,13 @@ __global__ void __launch_bounds__(NT) logprob_bwd_kernel(const LogprobArgs a) {
         }
       }
     }
-    __syncthreads();  // mark and the partial sums are reused by the next row
+    __syncthreads();  // the partial sums are reused by the next row; the targets' elements come after the others
+    if (grp && any)
+      for (int m = row.m0 + t; m < row.m1; m += NT) {
+        int tok;
+        float d;
+        if (first_token(m, tok, d)) dx[tok] = (T)a.target[m];  // members with one token write the same
+      }
   }
 }
 
@@ -511,7 +534,7 @@ __device__ __forceinline__ void policy_count(bool on, int m, int* count) {
 // The whole loss in one workgroup and launch, for few tokens and grouping arrays that fit LDS: five thousand tokens are
 // launches and dependent loads, no work.
 __global__ void __launch_bounds__(kPolicyThreads) policy_small_kernel(const PolicyArgs a) {
-  __shared__ int cu[kLdsMembers + 1], cnt[kLdsMembers + 1];
+  __shared__ int cu[kLdsMembers + 1], cnt[kLdsMembers + 1], first[kLdsGroups + 1];
   __shared__ double mw[kLdsMembers], tmp[kPolicyThreads / 64][4];
   __shared__ int tot[1][kPlanThreads / 64];
   __shared__ int bad, groups;
@@ -557,7 +580,12 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_small_kernel(const Poli
   __syncthreads();
   if (t == 0) a.hdr->error = bad;
   if (bad) return;
-  for (int m = start[0]; m < start[0] + members; ++m) mw[m] = (double)groups * (double)members;
+  if (t <= a.ng) first[t] = start[0];
+  __syncthreads();
+  for (int m = t; m < a.ns; m += kPolicyThreads) {
+    const int g = upper_index(first, 0, a.ng, m);  // of groups that start alike, the last has the members
+    mw[m] = (double)groups * (double)(first[g + 1] - first[g]);
+  }
   int mem[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
@@ -591,6 +619,7 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_small_kernel(const Poli
 __global__ void __launch_bounds__(kPolicyThreads) policy_plan_kernel(const PolicyArgs a) {
   __shared__ long long tmp[kPolicyThreads];
   __shared__ long long members;
+  __shared__ int first[kPolicyThreads + 1];
   __shared__ int bad, groups;
   const int t = threadIdx.x;
   if (t == 0) {
@@ -619,11 +648,19 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_plan_kernel(const Polic
   for (int base = 0; base < a.ng && !bad; base += kPolicyThreads) {
     const int g = base + t;
     const long long v = g < a.ng ? a.gsz[g] : 0;
-    const long long end = members + block_inclusive_scan<kPolicyThreads>(v, tmp);
-    if (g < a.ng && end <= a.ns)
-      for (long long m = end - v; m < end; ++m) a.member_w[m] = 1.0 / ((double)groups * (double)v);
+    const long long from = members, end = from + block_inclusive_scan<kPolicyThreads>(v, tmp);
+    // first member of each group of these, past the last member where sizes add up to more
+    first[t] = (int)min(end - v, (long long)a.ns);
+    if (t == kPolicyThreads - 1) {
+      first[kPolicyThreads] = (int)min(end, (long long)a.ns);
+      members = end;
+    }
     __syncthreads();
-    if (t == kPolicyThreads - 1) members = end;
+    for (int m = (int)min(from, (long long)a.ns) + t; m < first[kPolicyThreads]; m += kPolicyThreads) {
+      // of groups that start alike, the last has the members
+      const int k = upper_index(first, 0, min(kPolicyThreads, a.ng - base), m);
+      a.member_w[m] = 1.0 / ((double)groups * (double)(first[k + 1] - first[k]));
+    }
     __syncthreads();
   }
   if (t == 0) {

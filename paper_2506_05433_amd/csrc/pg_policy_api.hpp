@@ -19,6 +19,19 @@ int check_logprobs(int dtype, int token_bytes, int ng, int ns, int tp, int ts, c
 
 bool unaligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
 
+struct LogprobLayout {
+  RopeLayout plan;
+  size_t target, total;
+};
+
+LogprobLayout logprob_layout(int ng, int ns) {
+  LogprobLayout L{};
+  L.plan = rope_layout(ng);
+  L.target = align_up(L.plan.total);
+  L.total = L.target + align_up(sizeof(float) * (size_t)(ns > 0 ? ns : 1));
+  return L;
+}
+
 template <typename T, int NT>
 void launch_logprobs(const pg::LogprobArgs& a, bool bwd, unsigned blocks, hipStream_t st) {
   if (bwd) {
@@ -30,7 +43,7 @@ void launch_logprobs(const pg::LogprobArgs& a, bool bwd, unsigned blocks, hipStr
 int run_logprobs(int dtype, const pg::LogprobArgs& a0, bool bwd, const int32_t* gsz, int tp, void* workspace,
                  size_t workspace_bytes, void* stream) {
   pg::LogprobArgs a = a0;
-  const RopeLayout L = rope_layout(a.ng);
+  const LogprobLayout L = logprob_layout(a.ng, a.ns);
   if (!workspace || workspace_bytes < L.total)
     return fail(PG_EWORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, L.total);
   int rc = device_ready();
@@ -38,11 +51,12 @@ int run_logprobs(int dtype, const pg::LogprobArgs& a0, bool bwd, const int32_t* 
   if (a.ng == 0) return PG_OK;
   hipStream_t st = (hipStream_t)stream;
   char* ws = (char*)workspace;
-  a.hdr = (const pg::PlanHeader*)(ws + L.hdr);
-  a.ginfo = (const pg::GroupInfoEx*)(ws + L.ginfo);
+  a.hdr = (const pg::PlanHeader*)(ws + L.plan.hdr);
+  a.ginfo = (const pg::GroupInfoEx*)(ws + L.plan.ginfo);
+  a.target = (float*)(ws + L.target);
   {
     Timed tp_(PG_K_PLAN, st);
-    if ((rc = launch_rope_plan(L, ws, a.ng, a.ns, tp, a.ts, a.cu_p, a.cu_s, gsz, st))) return rc;
+    if ((rc = launch_rope_plan(L.plan, ws, a.ng, a.ns, tp, a.ts, a.cu_p, a.cu_s, gsz, st))) return rc;
   }
   if (!bwd && a.ts == 0) return PG_OK;  // no token to predict: no logits are read, they may be NULL
   // Threads a row, by its 16-byte pieces. 64: short rows where there are many, no barriers (5k rows, bf16: 1000 wide 8.8
@@ -93,7 +107,7 @@ extern "C" {
 
 size_t pg_token_logprobs_workspace_size(int n_groups, int n_suffixes, int total_suffix, int vocab) {
   if (n_groups < 0 || n_suffixes < 0 || total_suffix < 0 || vocab < 0) return 0;
-  return rope_layout(n_groups).total;
+  return logprob_layout(n_groups, n_suffixes).total;
 }
 
 int pg_token_logprobs(int dtype, int token_bytes, int n_groups, int n_suffixes, int total_prefix, int total_suffix,

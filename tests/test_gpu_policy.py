@@ -426,3 +426,65 @@ def test_rows_of_the_lowest_value_divided_by_a_temperature(dt):
     u = U[dt] + 2.0 ** -21  # the result's rounding; w, p and the target's sum, three of fp32
     assert (np.abs(gs[0].double().cpu().numpy() - want / temp) <= u * np.abs(want) / temp).all()
     assert bool((gs[1] == 0).all())
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("vocab", [37, 9001])
+def test_a_row_with_thousands_of_targets(dt, vocab):
+    """One group of more members than a workgroup keeps at hand, some of them empty, many with the same first token."""
+    from paper_2506_05433_amd import binding
+    rng = np.random.default_rng(vocab)
+    size = 2311
+    lens = ((3,), (size,), tuple(int(x) for x in rng.integers(0, 3, size)))
+    ts = sum(lens[2])
+    print(f"[logprobs] {size} members, {ts} rows, vocab {vocab} {dt}", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    last, _ = _logits(1, vocab, 0, 0, dt, gen)
+    suf, _ = _logits(ts, vocab, 0, 0, dt, gen)
+    tok = torch.randint(0, min(vocab, 1500), (ts,), generator=gen, device="cuda")
+    tok[::7] = -1
+    d = torch.randn(ts, generator=gen, device="cuda")
+    d[::5] = 0.0
+    g = _grp(lens)
+    _, lse = binding.token_logprobs(last, suf, tok, *g, 3)
+    gl, gs = binding.token_logprobs_bwd(last, suf, tok, lse, d, *g, 3)
+    dn, tn, at = d.double().cpu().numpy(), tok.cpu().numpy(), np.concatenate([[0], np.cumsum(lens[2])])
+    firsts = [r for r, s in zip(at, lens[2]) if s > 0 and tn[r] >= 0]
+    x = to_host(last)[0].astype(np.float64)
+    p = np.exp(x - x.max())
+    p /= p.sum()
+    add, mag = np.zeros(vocab), np.zeros(vocab)
+    np.add.at(add, tn[firsts], dn[firsts])
+    np.add.at(mag, tn[firsts], np.abs(dn[firsts]))
+    want = add - dn[firsts].sum() * p
+    # sums of at most n terms: n 2^-24 of the terms' magnitudes; p: its argument's error, as at the top; one fused product
+    n, zmax = len(firsts), np.abs(x).max()
+    ptol = 2.0 ** -23 * (2 * zmax + 8) + 2.0 ** -22 * (zmax + vocab / 256 + 40)
+    lim = n * 2.0 ** -24 * (mag + mag.sum() * p) + (ptol + 2.0 ** -23) * mag.sum() * p + 1.01 * U[dt] * np.abs(want)
+    lim += U[dt] * lim + 2.0 ** -23 * mag
+    err = np.abs(to_host(gl)[0].astype(np.float64) - want)
+    assert (err <= lim).all(), (err / lim).max()
+    # the policy loss over that group: weights 1 / (members x tokens)
+    adv = torch.randn(size, generator=gen, device="cuda")
+    stats, dl = binding.policy_loss(d, adv, g[1], g[2])
+    sizes = np.array(lens[2])
+    w = np.repeat(1.0 / (size * np.maximum(sizes, 1)), sizes)
+    a = np.repeat(adv.double().cpu().numpy(), sizes)
+    assert (np.abs(dl.double().cpu().numpy() + w * a) <= 2.0 ** -24 * np.abs(w * a) + 1e-14).all()
+    assert abs(stats[0].item() + (w * a).sum()) <= 2.0 ** -24 * abs((w * a).sum()) + 1e-12
+
+
+def test_policy_loss_of_many_groups():
+    """More groups than the planner takes at a time, some without members, and more tokens than one workgroup takes."""
+    from paper_2506_05433_amd import binding
+    rng = np.random.default_rng(8)
+    groups = rng.integers(0, 4, 2500)
+    sizes = rng.integers(0, 6, groups.sum())
+    ts = int(sizes.sum())
+    assert ts > 8192
+    adv = torch.from_numpy(rng.standard_normal(len(sizes)).astype(np.float32)).cuda()
+    stats, dl = binding.policy_loss(torch.zeros(ts, device="cuda"), adv, _cu(sizes), torch.tensor(groups, dtype=torch.int32, device="cuda"))
+    w = np.repeat(1.0 / ((groups > 0).sum() * np.repeat(groups, groups) * np.maximum(sizes, 1)), sizes)
+    a = np.repeat(adv.double().cpu().numpy(), sizes)
+    assert (np.abs(dl.double().cpu().numpy() + w * a) <= 2.0 ** -24 * np.abs(w * a) + 1e-14).all()
+    assert abs(stats[0].item() + (w * a).sum()) <= 2.0 ** -24 * abs((w * a).sum()) + 1e-12
