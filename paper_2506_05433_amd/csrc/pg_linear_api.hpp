@@ -39,11 +39,12 @@ ItemRows linear_item_rows(int ns, int tp, int ts, int h_q, int h_kv, int d, bool
     return r;
   }
   // output workgroups take all query heads of a kv head (or a divisor of their number) while there are 512 of them
-  // with 64-row items: they share the state's updates, keys and values. P 4096, 8 x 256..1024 rows, 32/8 heads: 1, 2
-  // and 4 heads 79, 57 and 52 us; 8100 rows, 16/4 heads, d 64: 25, 22 and 18
+  // with 64-row items, one for each member at least: they share the state's updates, keys and values. P 4096, 8 x
+  // 256..1024 rows, 32/8 heads: 1, 2 and 4 heads 79, 57 and 52 us; 8100 rows, 16/4 heads, d 64: 25, 22 and 18; P 1024,
+  // 256 x 1 row, 32/8 heads, the whole forward with 1 and 4: 115 and 77
   if (!grad)
     for (int n = 1; n <= ratio; ++n)
-      if (ratio % n == 0 && rows * h_kv * (ratio / n) >= 512L * 64) r.hpw = n;
+      if (ratio % n == 0 && std::max(rows, 64L * ns) * h_kv * (ratio / n) >= 512L * 64) r.hpw = n;
   const int heads = grad ? h_kv : h_q / r.hpw;
   // members: whole where there are enough of them (up to twice the mean length: a longer one is split), else about 512
   // workgroups in all; a chunk at least
