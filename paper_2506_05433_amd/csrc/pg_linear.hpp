@@ -429,11 +429,11 @@ template <typename T, int D>
 using LinStateTiles = LinTiles<T, D, D == 128 && sizeof(T) == 4 ? 32 : 64, 4>;
 constexpr int kLinStateThreads = 256;
 template <typename T, int D, bool REV, int SPLIT>
-__global__ void __launch_bounds__(kLinStateThreads, 2) lin_state_kernel(const LinArgs a) {
+__device__ __forceinline__ void lin_state_walk(const LinArgs& a, unsigned block,
+                                               char (&lds)[2][2 * LinStateTiles<T, D>::kTileBytes]) {
   using S = LinStateTiles<T, D>;
   static_assert(S::kNT == kLinStateThreads, "threads");
-  __shared__ __align__(16) char lds[2][2 * S::kTileBytes];
-  const BlockSlot slot = xcd_slot(blockIdx.x, a.h_kv, 1);
+  const BlockSlot slot = xcd_slot(block, a.h_kv, 1);
   if (slot.unit >= a.max_items) return;
   const LinItem it = uniform_item(a.items, slot.unit);  // loaded beside the number of items, not behind it
   if (slot.unit >= *a.n_items) return;
@@ -478,9 +478,18 @@ __global__ void __launch_bounds__(kLinStateThreads, 2) lin_state_kernel(const Li
   state_store<D>(acc, a.slots + ((size_t)it.self * a.h_kv + kv) * (size_t)(D * D), kb0, nb, lane);
 }
 
+// One walk's items, or (`first` > 0) those of both walks of a backward call: `first` workgroups of the reverse one, r's,
+// which reads more, then the forward one's.
+template <typename T, int D, int SPLIT>
+__global__ void __launch_bounds__(kLinStateThreads, 2) lin_state_kernel(const LinArgs a, const LinArgs r, unsigned first) {
+  __shared__ __align__(16) char lds[2][2 * LinStateTiles<T, D>::kTileBytes];
+  if (blockIdx.x < first) lin_state_walk<T, D, true, SPLIT>(r, blockIdx.x, lds);
+  else lin_state_walk<T, D, false, SPLIT>(a, blockIdx.x - first, lds);
+}
+
 // ---------------------------------------------------------------- scans
 // In place over a segment's items: slot := l^rows (state before) + own share. Prefixes (PART 0) and members (PART 1)
-// are separate launches, members first in a backward walk; grid (D * D / (256 V::kN), h_kv, segments). Chains of
+// follow one another, members first in a backward walk; D * D / (256 V::kN) workgroups a kv head and segment. Chains of
 // dependent sums, all latency, so a thread has kBatch loads in flight. A prefix has many items and there are few
 // prefixes: one entry a thread, 32 loads; members have few items or none to do: four entries a thread, 8 loads, fewer
 // workgroups (P 16384 in 32 items, 16 members summed: 53 -> 16 us; 64 members with nothing to do 17 -> 6 us).
@@ -496,18 +505,29 @@ struct ScanVec<1> {
   static constexpr int kN = 4, kBatch = 8;
 };
 
+// segments and workgroups that a scan has side by side
+template <int D, int PART>
+__host__ __device__ inline int scan_segs(const LinArgs& a) {
+  const int most = (1 << 20) / (D * D / (kScanThreads * ScanVec<PART>::kN) * a.h_kv), segs = PART ? a.ns : a.ng;
+  return segs < most ? segs : most;
+}
+template <int D, int PART>
+__host__ __device__ inline unsigned scan_blocks(const LinArgs& a) {
+  return D * D / (kScanThreads * ScanVec<PART>::kN) * a.h_kv * scan_segs<D, PART>(a);
+}
+
 template <int D, bool REV, int PART>
-__global__ void __launch_bounds__(kScanThreads) lin_scan_kernel(const LinArgs a) {
+__device__ __forceinline__ void lin_scan(const LinArgs& a, unsigned block) {
   using S = ScanVec<PART>;
   using V = typename S::type;
-  constexpr int kBatch = S::kBatch;
-  const int kv = blockIdx.y;
-  const size_t e = S::kN * ((size_t)blockIdx.x * kScanThreads + threadIdx.x), per = (size_t)D * D;
+  constexpr int kBatch = S::kBatch, kParts = D * D / (kScanThreads * S::kN);
+  const int kv = block / kParts % a.h_kv, seg0 = block / kParts / a.h_kv, step = scan_segs<D, PART>(a);
+  const size_t e = S::kN * ((size_t)(block % kParts) * kScanThreads + threadIdx.x), per = (size_t)D * D;
   const float g = log2_decay(a.log_decay, kv);
   auto at = [&](int slot) { return (V*)(a.slots + ((size_t)slot * a.h_kv + kv) * per + e); };
   auto user = [&](const float* p, int seg) { return (V*)(p + ((size_t)seg * a.h_kv + kv) * per + e); };
   const float full = fast_exp2(g * (float)(PART ? a.l_suf : a.l_pre));  // the rows of all items but a segment's last
-  for (int seg = blockIdx.z; seg < (PART ? a.ns : a.ng); seg += gridDim.z) {
+  for (int seg = seg0; seg < (PART ? a.ns : a.ng); seg += step) {
     const int s = PART ? a.ng + seg : seg;
     const int i0 = a.seg_off[s], i1 = a.seg_off[s + 1];
     // the last item holds what the others leave
@@ -568,6 +588,14 @@ __global__ void __launch_bounds__(kScanThreads) lin_scan_kernel(const LinArgs a)
   }
 }
 
+// Scans of the first kind (a forward walk's prefixes, a reverse one's members) or the second, of the walks that come:
+// `first` workgroups for a, the forward walk, the others for r.
+template <int D, bool SECOND>
+__global__ void __launch_bounds__(kScanThreads) lin_scan_kernel(const LinArgs a, const LinArgs r, unsigned first) {
+  if (blockIdx.x < first) lin_scan<D, false, SECOND ? 1 : 0>(a, blockIdx.x);
+  else lin_scan<D, true, SECOND ? 0 : 1>(r, blockIdx.x - first);
+}
+
 // ---------------------------------------------------------------- outputs (and dq, with the roles swapped)
 // One workgroup: one item and `hpw` of the query heads of one kv head, which share the keys, the values and the state
 // in LDS. Wave w: query rows 32 (w % kNQ).. of each chunk, columns 32 kDT (w / kNQ).. of the output. Queries come and
@@ -576,15 +604,17 @@ template <typename T, int D>
 using LinOutTiles = LinTiles<T, D, D == 128 ? 32 : 64, 4>;
 constexpr int kLinThreads = 256;
 
+template <typename T, int D>
+constexpr int kLinLds = 4 * LinOutTiles<T, D>::kTileBytes + LinOutTiles<T, D>::kStateBytes;
+
 template <typename T, int D, int SPLIT>
-__global__ void __launch_bounds__(kLinThreads, sizeof(T) == 2 ? 2 : 1) lin_out_kernel(const LinArgs a, int hpw) {
+__device__ __forceinline__ void lin_out(const LinArgs& a, int hpw, unsigned block, char (&lds)[kLinLds<T, D>]) {
   using S = LinOutTiles<T, D>;
   using E = Elt<T>;
   static_assert(S::kNT == kLinThreads, "threads");
   constexpr int kDT = S::kNB / (S::kNW / S::kNQ), kKK = D / 16;
-  __shared__ __align__(16) char lds[4 * S::kTileBytes + S::kStateBytes];
   const int ratio = a.h_q / a.h_kv, parts = ratio / hpw;
-  const BlockSlot slot = xcd_slot(blockIdx.x, a.h_kv * parts, parts);
+  const BlockSlot slot = xcd_slot(block, a.h_kv * parts, parts);
   if (slot.unit >= a.max_items) return;
   const LinItem it = uniform_item(a.items, slot.unit);  // loaded beside the number of items, not behind it
   if (slot.unit >= *a.n_items) return;
@@ -696,21 +726,22 @@ __global__ void __launch_bounds__(kLinThreads, sizeof(T) == 2 ? 2 : 1) lin_out_k
   if (keep) state_store<D>(acc, a.state_out[1] + ((size_t)it.seg * a.h_kv + kv) * (size_t)(D * D), kb0, nb, lane);
 }
 
+template <typename T, int D, int SPLIT>
+__global__ void __launch_bounds__(kLinThreads, sizeof(T) == 2 ? 2 : 1) lin_out_kernel(const LinArgs a, int hpw) {
+  __shared__ __align__(16) char lds[kLinLds<T, D>];
+  lin_out<T, D, SPLIT>(a, hpw, blockIdx.x, lds);
+}
+
 // ---------------------------------------------------------------- dk, dv
 // One workgroup: one item, one kv head, walked backwards; the query heads that share it follow one another in each
 // chunk. Wave w: key rows 32 (w % kNQ).., and of the kNW / kNQ others the first half dv, the second dk, kWT tiles of
 // columns each. Everything passes LDS in whole rows; what the next head or chunk needs is loaded to registers meanwhile.
-template <typename T, int D>
-using LinGradTiles = LinTiles<T, D, D == 128 ? 32 : 64, 4>;
-
 template <typename T, int D, int SPLIT>
-__global__ void __launch_bounds__(kLinThreads, sizeof(T) == 2 ? 2 : 1) lin_grad_kernel(const LinArgs a, int only) {
-  using S = LinGradTiles<T, D>;
+__device__ __forceinline__ void lin_grad(const LinArgs& a, int only, unsigned block, char (&lds)[kLinLds<T, D>]) {
+  using S = LinOutTiles<T, D>;
   using E = Elt<T>;
-  static_assert(S::kNT == kLinThreads, "threads");
   constexpr int kParts = S::kNW / S::kNQ, kWT = S::kNB / (kParts / 2), kKK = D / 16;
-  __shared__ __align__(16) char lds[4 * S::kTileBytes + S::kStateBytes];
-  const BlockSlot slot = xcd_slot(blockIdx.x, a.h_kv, 1);
+  const BlockSlot slot = xcd_slot(block, a.h_kv, 1);
   if (slot.unit >= a.max_items) return;
   const LinItem it = uniform_item(a.items, slot.unit);  // loaded beside the number of items, not behind it
   if (slot.unit >= *a.n_items) return;
@@ -836,6 +867,22 @@ __global__ void __launch_bounds__(kLinThreads, sizeof(T) == 2 ? 2 : 1) lin_grad_
     __syncthreads();
   }
   if (keep) state_store<D>(acc, a.slots + ((size_t)it.self * a.h_kv + kv) * (size_t)(D * D), kb0, nb, lane);
+}
+
+template <typename T, int D, int SPLIT>
+__global__ void __launch_bounds__(kLinThreads, sizeof(T) == 2 ? 2 : 1) lin_grad_kernel(const LinArgs a, int only) {
+  __shared__ __align__(16) char lds[kLinLds<T, D>];
+  lin_grad<T, D, SPLIT>(a, only, blockIdx.x, lds);
+}
+
+// dk and dv (`first` workgroups, of g) and dq in one launch, where no order between the items is needed: the longer
+// workgroups first.
+template <typename T, int D, int SPLIT>
+__global__ void __launch_bounds__(kLinThreads, sizeof(T) == 2 ? 2 : 1) lin_grads_kernel(const LinArgs dq, int hpw,
+                                                                                       const LinArgs g, unsigned first) {
+  __shared__ __align__(16) char lds[kLinLds<T, D>];
+  if (blockIdx.x < first) lin_grad<T, D, SPLIT>(g, -1, blockIdx.x, lds);
+  else lin_out<T, D, SPLIT>(dq, hpw, blockIdx.x - first, lds);
 }
 
 // ---------------------------------------------------------------- single tokens

@@ -72,9 +72,9 @@ struct LinearLayout {
   struct List {
     ItemRows rows;
     int max_items;
-    size_t seg_off, items;
+    size_t seg_off, items, slots;
   };
-  size_t hdr, ginfo, qoff, kvoff, slots, total;
+  size_t hdr, ginfo, qoff, kvoff, total;
   List out, grad;  // the forward walk (outputs, or dq); the backward one (dk, dv)
 };
 
@@ -88,7 +88,6 @@ LinearLayout linear_layout(int dtype, int ng, int ns, int tp, int ts, int h_q, i
   L.ginfo = take(sizeof(pg::GroupInfoEx) * (size_t)(ng > 0 ? ng : 1));
   L.qoff = take(sizeof(int) * ((size_t)ng + 1));
   L.kvoff = take(sizeof(int) * ((size_t)ng + 1));
-  long most = 0;
   auto list = [&](LinearLayout::List& l, bool grad) {
     const bool alone = dtype >= 0 && linear_alone(dtype, tp, ts, h_q / h_kv, d, grad);
     l.rows = linear_item_rows(ns, tp, ts, h_q, h_kv, d, grad, alone);
@@ -97,22 +96,12 @@ LinearLayout linear_layout(int dtype, int ng, int ns, int tp, int ts, int h_q, i
     l.max_items = items > INT32_MAX ? -1 : (int)items;
     l.seg_off = take(sizeof(int) * ((size_t)ng + ns + 1));
     l.items = take(sizeof(pg::LinItem) * (size_t)items);
-    most = std::max(most, items);
+    l.slots = take(sizeof(float) * (size_t)(items + ng) * h_kv * d * d);
   };
   list(L.out, false);
   if (bwd) list(L.grad, true);
-  L.slots = take(sizeof(float) * (size_t)(most + ng) * h_kv * d * d);  // the walks follow one another
   L.total = off;
   return L;
-}
-
-template <int D, bool REV, int PART>
-void linear_scan(const Common& c, const pg::LinArgs& a, hipStream_t st) {
-  const int segs = PART ? c.ns : c.ng;
-  if (segs > 0)
-    hipLaunchKernelGGL((pg::lin_scan_kernel<D, REV, PART>),
-                       dim3(D * D / (pg::kScanThreads * pg::ScanVec<PART>::kN), c.h_kv, std::min(segs, 65535)),
-                       dim3(pg::kScanThreads), 0, st, a);
 }
 
 // Groups and items of the call's walks.
@@ -140,27 +129,34 @@ int linear_plan(const Common& c, const LinearLayout& L, char* ws, const int32_t*
   return PG_OK;
 }
 
-// The items' own shares of one walk.
-template <typename T, int D, bool REV, int SPLIT>
-void linear_states(const Common& c, const pg::LinArgs& a, hipStream_t st) {
-  const long blocks = pg::xcd_grid_blocks(a.max_items, c.h_kv, 1);
-  hipLaunchKernelGGL((pg::lin_state_kernel<T, D, REV, SPLIT>), dim3((unsigned)blocks), dim3(pg::kLinStateThreads), 0,
-                     st, a);
+// States before the items of a forward walk and, in a backward call, of its reverse walk (either may be NULL): shares and
+// scans of both side by side. The prefixes' scan of a members_first walk comes later.
+template <typename T, int D, int SPLIT>
+void linear_states(const Common& c, const pg::LinArgs* a, const pg::LinArgs* r, hipStream_t st) {
+  if (!a && !r) return;
+  Timed tm(PG_K_LINEAR_STATE, st);
+  const pg::LinArgs &fa = a ? *a : *r, &fr = r ? *r : *a;
+  auto blocks = [&](const pg::LinArgs* w) { return w ? (unsigned)pg::xcd_grid_blocks(w->max_items, c.h_kv, 1) : 0u; };
+  hipLaunchKernelGGL((pg::lin_state_kernel<T, D, SPLIT>), dim3(blocks(a) + blocks(r)), dim3(pg::kLinStateThreads), 0, st,
+                     fa, fr, blocks(r));
+  const unsigned a1 = a ? pg::scan_blocks<D, 0>(*a) : 0, r1 = r ? pg::scan_blocks<D, 1>(*r) : 0;
+  if (a1 + r1)
+    hipLaunchKernelGGL((pg::lin_scan_kernel<D, false>), dim3(a1 + r1), dim3(pg::kScanThreads), 0, st, fa, fr, a1);
+  const unsigned a2 = a ? pg::scan_blocks<D, 1>(*a) : 0, r2 = r && !r->members_first ? pg::scan_blocks<D, 0>(*r) : 0;
+  if (a2 + r2)
+    hipLaunchKernelGGL((pg::lin_scan_kernel<D, true>), dim3(a2 + r2), dim3(pg::kScanThreads), 0, st, fa, fr, a2);
 }
 
-// The forward walk: shares, scans (prefixes, then the members that start from them), outputs.
-template <typename T, int D, int SPLIT>
-void linear_walk(const Common& c, int hpw, const pg::LinArgs& a, hipStream_t st) {
-  if (!a.alone) {
-    Timed tm(PG_K_LINEAR_STATE, st);
-    linear_states<T, D, false, SPLIT>(c, a, st);
-    linear_scan<D, false, 0>(c, a, st);
-    linear_scan<D, false, 1>(c, a, st);
-  }
-  Timed tm(PG_K_LINEAR_OUT, st);
+unsigned linear_out_blocks(const Common& c, int hpw, const pg::LinArgs& a) {
   const int parts = c.h_q / c.h_kv / hpw;
-  const long blocks = pg::xcd_grid_blocks(a.max_items, c.h_kv * parts, parts);
-  hipLaunchKernelGGL((pg::lin_out_kernel<T, D, SPLIT>), dim3((unsigned)blocks), dim3(pg::kLinThreads), 0, st, a, hpw);
+  return (unsigned)pg::xcd_grid_blocks(a.max_items, c.h_kv * parts, parts);
+}
+
+template <typename T, int D, int SPLIT>
+void linear_outputs(const Common& c, int hpw, const pg::LinArgs& a, hipStream_t st) {
+  Timed tm(PG_K_LINEAR_OUT, st);
+  hipLaunchKernelGGL((pg::lin_out_kernel<T, D, SPLIT>), dim3(linear_out_blocks(c, hpw, a)), dim3(pg::kLinThreads), 0, st,
+                     a, hpw);
 }
 
 void linear_common_args(pg::LinArgs& a, const Common& c, const LinearLayout& L, bool grad, char* ws,
@@ -168,7 +164,7 @@ void linear_common_args(pg::LinArgs& a, const Common& c, const LinearLayout& L, 
   const LinearLayout::List& l = grad ? L.grad : L.out;
   a.log_decay = log_decay;
   a.cu_p = cu_p; a.cu_s = cu_s;
-  a.slots = (float*)(ws + L.slots);
+  a.slots = (float*)(ws + l.slots);
   a.seg_off = (const int*)(ws + l.seg_off);
   a.items = (const pg::LinItem*)(ws + l.items);
   a.hdr = (const pg::PlanHeader*)(ws + L.hdr);
@@ -181,6 +177,12 @@ void linear_common_args(pg::LinArgs& a, const Common& c, const LinearLayout& L, 
   a.scale = c.scale;
 }
 
+template <typename T, int D, int SPLIT>
+void linear_walk(const Common& c, int hpw, const pg::LinArgs& a, hipStream_t st) {
+  linear_states<T, D, SPLIT>(c, a.alone ? nullptr : &a, nullptr, st);
+  linear_outputs<T, D, SPLIT>(c, hpw, a, st);
+}
+
 template <typename T, int D>
 void linear_fwd_typed(const Common& c, int hpw, const pg::LinArgs& a, hipStream_t st) {
   constexpr bool b16 = sizeof(T) == 2;
@@ -191,32 +193,33 @@ void linear_fwd_typed(const Common& c, int hpw, const pg::LinArgs& a, hipStream_
 template <typename T, int D>
 void linear_bwd_typed(const Common& c, int hpw, const pg::LinArgs& dq, const pg::LinArgs& g, hipStream_t st) {
   constexpr int SPLIT = sizeof(T) == 2 ? 2 : 1;
-  linear_walk<T, D, SPLIT>(c, hpw, dq, st);
+  linear_states<T, D, SPLIT>(c, dq.alone ? nullptr : &dq, g.alone ? nullptr : &g, st);
+  const unsigned first = (unsigned)pg::xcd_grid_blocks(g.max_items, c.h_kv, 1);
+  if (!g.members_first) {
+    Timed tm(PG_K_LINEAR_GRAD, st);
+    hipLaunchKernelGGL((pg::lin_grads_kernel<T, D, SPLIT>), dim3(first + linear_out_blocks(c, hpw, dq)),
+                       dim3(pg::kLinThreads), 0, st, dq, hpw, g, first);
+    return;
+  }
+  linear_outputs<T, D, SPLIT>(c, hpw, dq, st);
+  // the members' walks end with the states that the prefixes' start from: no pass over the responses for them alone
   auto grad = [&](int part) {
     Timed tm(PG_K_LINEAR_GRAD, st);
-    const long blocks = pg::xcd_grid_blocks(g.max_items, c.h_kv, 1);
-    hipLaunchKernelGGL((pg::lin_grad_kernel<T, D, SPLIT>), dim3((unsigned)blocks), dim3(pg::kLinThreads), 0, st, g, part);
+    hipLaunchKernelGGL((pg::lin_grad_kernel<T, D, SPLIT>), dim3(first), dim3(pg::kLinThreads), 0, st, g, part);
   };
-  if (!g.alone) {
-    Timed tm(PG_K_LINEAR_STATE, st);
-    linear_states<T, D, true, SPLIT>(c, g, st);
-    linear_scan<D, true, 1>(c, g, st);
-    if (!g.members_first) linear_scan<D, true, 0>(c, g, st);
-  }
-  if (!g.members_first) return grad(-1);
-  // the members' walks end with the states that the prefixes' start from: no pass over the responses for them alone
   grad(1);
   {
     Timed tm(PG_K_LINEAR_STATE, st);
-    linear_scan<D, true, 0>(c, g, st);
+    hipLaunchKernelGGL((pg::lin_scan_kernel<D, true>), dim3(pg::scan_blocks<D, 0>(g)), dim3(pg::kScanThreads), 0, st, g, g,
+                       0u);
   }
   grad(0);
 }
 
-int linear_grid_check(const Common& c, const LinearLayout::List& l) {
+// items: of all walks of the call
+int linear_grid_check(const Common& c, long items) {
   // workgroups of 256 threads, fewer than 2^32 threads a launch; item and slot numbers in 31 bits
-  if (l.max_items < 0 || (long)l.max_items + c.ng > INT32_MAX || ((long)l.max_items + 8) * c.h_q * 256 > 0xffffffffL ||
-      c.h_kv > 65535)
+  if (items < 0 || items + c.ng > INT32_MAX || (items + 16) * c.h_q * 256 > 0xffffffffL)
     return fail(PG_EUNSUPPORTED, "%d groups, %d members x %d heads exceed the launch grid", c.ng, c.ns, c.h_q);
   return PG_OK;
 }
@@ -268,7 +271,7 @@ int pg_linear_fwd(int dtype, int n_groups, int n_suffixes, int total_prefix, int
   if (overlap(state_in, state_pre, in, in) || overlap(state_in, state_suf, in, state * n_suffixes))
     return fail(PG_EINVAL, "state_in overlaps state_pre or state_suf");
   const LinearLayout L = linear_layout(state_pre || state_suf ? -1 : dtype, c.ng, c.ns, c.tp, c.ts, c.h_q, c.h_kv, c.d, false);
-  if ((rc = linear_grid_check(c, L.out))) return rc;
+  if ((rc = linear_grid_check(c, L.out.max_items))) return rc;
   if (!workspace || workspace_bytes < L.total)
     return fail(PG_EWORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, L.total);
   if ((rc = device_ready())) return rc;
@@ -312,7 +315,8 @@ int pg_linear_bwd(int dtype, int n_groups, int n_suffixes, int total_prefix, int
                   dv_suf, workspace}))
     return fail(PG_EINVAL, "tensor pointers must be 16-byte aligned");
   const LinearLayout L = linear_layout(dtype, c.ng, c.ns, c.tp, c.ts, c.h_q, c.h_kv, c.d, true);
-  if ((rc = linear_grid_check(c, L.out)) || (rc = linear_grid_check(c, L.grad))) return rc;
+  const long items = L.out.max_items < 0 || L.grad.max_items < 0 ? -1 : (long)L.out.max_items + L.grad.max_items;
+  if ((rc = linear_grid_check(c, items))) return rc;
   if (!workspace || workspace_bytes < L.total)
     return fail(PG_EWORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, L.total);
   if ((rc = device_ready())) return rc;
