@@ -875,13 +875,14 @@ __global__ void __launch_bounds__(kLinThreads, sizeof(T) == 2 ? 2 : 1) lin_grad_
   lin_grad<T, D, SPLIT>(a, only, blockIdx.x, lds);
 }
 
-// dk and dv (`first` workgroups, of g) and dq in one launch, where no order between the items is needed: the longer
-// workgroups first.
+// dk and dv (`first` workgroups, of g) and dq in one launch, the longer workgroups first: one does not wait for the
+// other's last ones.
 template <typename T, int D, int SPLIT>
 __global__ void __launch_bounds__(kLinThreads, sizeof(T) == 2 ? 2 : 1) lin_grads_kernel(const LinArgs dq, int hpw,
-                                                                                       const LinArgs g, unsigned first) {
+                                                                                       const LinArgs g, unsigned first,
+                                                                                       int only) {
   __shared__ __align__(16) char lds[kLinLds<T, D>];
-  if (blockIdx.x < first) lin_grad<T, D, SPLIT>(g, -1, blockIdx.x, lds);
+  if (blockIdx.x < first) lin_grad<T, D, SPLIT>(g, only, blockIdx.x, lds);
   else lin_out<T, D, SPLIT>(dq, hpw, blockIdx.x - first, lds);
 }
 

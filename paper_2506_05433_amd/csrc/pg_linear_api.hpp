@@ -195,25 +195,20 @@ void linear_bwd_typed(const Common& c, int hpw, const pg::LinArgs& dq, const pg:
   constexpr int SPLIT = sizeof(T) == 2 ? 2 : 1;
   linear_states<T, D, SPLIT>(c, dq.alone ? nullptr : &dq, g.alone ? nullptr : &g, st);
   const unsigned first = (unsigned)pg::xcd_grid_blocks(g.max_items, c.h_kv, 1);
-  if (!g.members_first) {
+  {
     Timed tm(PG_K_LINEAR_GRAD, st);
     hipLaunchKernelGGL((pg::lin_grads_kernel<T, D, SPLIT>), dim3(first + linear_out_blocks(c, hpw, dq)),
-                       dim3(pg::kLinThreads), 0, st, dq, hpw, g, first);
-    return;
+                       dim3(pg::kLinThreads), 0, st, dq, hpw, g, first, g.members_first ? 1 : -1);
   }
-  linear_outputs<T, D, SPLIT>(c, hpw, dq, st);
-  // the members' walks end with the states that the prefixes' start from: no pass over the responses for them alone
-  auto grad = [&](int part) {
-    Timed tm(PG_K_LINEAR_GRAD, st);
-    hipLaunchKernelGGL((pg::lin_grad_kernel<T, D, SPLIT>), dim3(first), dim3(pg::kLinThreads), 0, st, g, part);
-  };
-  grad(1);
+  if (!g.members_first) return;
+  // the members' walks have ended with the states that the prefixes' start from: no pass over the responses for them alone
   {
     Timed tm(PG_K_LINEAR_STATE, st);
     hipLaunchKernelGGL((pg::lin_scan_kernel<D, true>), dim3(pg::scan_blocks<D, 0>(g)), dim3(pg::kScanThreads), 0, st, g, g,
                        0u);
   }
-  grad(0);
+  Timed tm(PG_K_LINEAR_GRAD, st);
+  hipLaunchKernelGGL((pg::lin_grad_kernel<T, D, SPLIT>), dim3(first), dim3(pg::kLinThreads), 0, st, g, 0);
 }
 
 // items: of all walks of the call
