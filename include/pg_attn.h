@@ -262,8 +262,9 @@ int pg_grouped_positions(int n_groups, int n_suffixes, int total_prefix, int tot
  * (either may be NULL) receive the states after each prefix and after each response (an empty response: its
  * prefix's), from which pg_linear_step goes on. They must not overlap state_in.
  *
- * The workspace of either direction holds a state (4 * head_dim^2 bytes a kv head) for each group, each member and
- * each further piece of a long segment (of 32 rows or more): 0.1 GB for 8 groups of 16 with 8 kv heads of 128.
+ * The forward's workspace holds a state (4 * head_dim^2 bytes a kv head) for each group, each member and each further
+ * piece of a long segment (of 32 rows or more), the backward's two: 0.1 and 0.2 GB for 8 groups of 16 with 8 kv heads of
+ * 128.
  */
 size_t pg_linear_fwd_workspace_size(int n_groups, int n_suffixes, int total_prefix, int total_suffix, int h_q,
                                     int h_kv, int head_dim);
@@ -381,9 +382,9 @@ typedef enum {
   PG_K_ROPE = 5,     /* rotary embedding kernel of pg_rope                    */
   PG_K_LAST = 6,     /* pg_attn_fwd_last: chunk kernel and merge, one interval */
   PG_K_KV_REDUCE = 7, /* backward: fixed-order sum of the prefix dK/dV partials */
-  PG_K_LINEAR_STATE = 8, /* linear attention: item plan, states and scans of one walk, one interval */
-  PG_K_LINEAR_OUT = 9,   /* linear attention: outputs, or dq                   */
-  PG_K_LINEAR_GRAD = 10, /* linear attention: dk, dv                           */
+  PG_K_LINEAR_STATE = 8, /* linear attention: states and scans between items   */
+  PG_K_LINEAR_OUT = 9,   /* linear attention: outputs                          */
+  PG_K_LINEAR_GRAD = 10, /* linear attention: dq, dk, dv                       */
   PG_K_LINEAR_STEP = 11, /* linear attention: single tokens                    */
   PG_K_LOGPROBS = 12,    /* token log-probabilities, or their gradient         */
   PG_K_POLICY = 13       /* policy loss: counts, terms and sums, one interval  */

@@ -14,12 +14,12 @@ struct ItemRows {
   int round;  // items that fill the CUs once, where they are ordered by length (pg_linear.hpp, item_place)
 };
 
-// Few rows are launches and latency: the state and scan kernels of both walks are 9 of a step's 14 launches. Where one
-// workgroup gets over the rows that its own start from faster than those kernels pass it the state, every segment is
-// one item, and a member's workgroup walks its prefix first (a prefix's its members, backwards). Measured, us alone
-// and in 32-row items, forward then backward: P 64, 4 x 24 rows, d 64, fp32 16, 22 and 35, 45; bf16 P 128, 4 x 16,
-// 8/2 heads 16, 20 and (dk, dv walk 192 rows x 4 heads) 54, 43; P 192 20, 21 and 81, 47; P 400 33, 23; fp32 d 128
-// P 128 36, 25.
+// Few rows are launches and latency: the states and scans are 3 of a call's 5 launches. Where one workgroup gets over the
+// rows that its own start from faster than those kernels pass it the state, every segment is one item, and a member's
+// workgroup walks its prefix first (a prefix's its members, backwards). Measured, us alone and in 32-row items, forward
+// then backward: P 64, 4 x 24 rows, d 64, fp32 15, 22 and 23, 28, bf16 10, 17 and 15, 21; bf16 d 128 P 128, 4 x 16, 8/2
+// heads 15, 19 and (dk, dv walk 192 rows x 4 heads) 54, 29; P 192 20, 20 and 81, 33; P 400 33, 22; fp32 d 128 P 128 36,
+// 24.
 constexpr int kAloneRows = 512;
 
 bool linear_alone(int dtype, int tp, int ts, int ratio, int d, bool grad) {
